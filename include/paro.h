@@ -280,6 +280,113 @@ int paro_sparse_attn_unpermuted_rawq(const paro_shape* s, paro_dtype q_dtype, in
                                      const int32_t* row_order, const uint8_t* h_perm_ids,
                                      paro_dtype out_dtype, void* o, void* stream);
 
+/* ---- norms of Q and K and their rotation by position, in front of the attention call --------------------------
+ * What a visual transformer does to Q and K between their projection and its attention: every head's row is divided
+ * by its norm, and channel pairs turn by angles that grow with the token's (frame, height, width) position.  The paper
+ * folds the reorder into this very step (App. C, "Overhead of Permutation").
+ *
+ * Rotation.  dims[0] channels turn with the frame coordinate of a token, the next dims[1] with the height, the next
+ * dims[2] with the width coordinate; channels behind those, and text tokens, are not turned.  Channels come in pairs:
+ * pair p is (2p, 2p+1) for PARO_PAIRS_ADJACENT and (p, p + d/2) for PARO_PAIRS_HALVES, p in [0, d/2); an axis owns
+ * dims[a]/2 consecutive pairs.  A pair (x, y) becomes (x c - y s, x s + y c) with c and s the cosine and sine of the
+ * token's coordinate along the pair's axis times the pair's frequency.
+ *
+ * The angles of a grid separate by axis, so the table holds them per coordinate and not per token: (cosine, sine) of
+ * coordinate i and pair p of an axis at entry i * dims[a]/2 + p, the axes' entries one behind the other, float32
+ * (13 x 30 x 45 tokens at d = 64: 8 KB, which stays in the caches nearest to a compute unit; 4.5 MB per token). */
+typedef enum paro_pairs { PARO_PAIRS_ADJACENT = 0, PARO_PAIRS_HALVES = 1 } paro_pairs;
+
+typedef struct paro_rope_axes {
+    int32_t dims[3]; /* channels turned by the frame, height and width coordinate: even, >= 0, together <= d */
+    int32_t pairs;   /* a paro_pairs */
+} paro_rope_axes;
+
+/* Numbers of the table (two per entry); a negative status on invalid arguments. */
+int64_t paro_rope_table_floats(const paro_shape* s, const paro_rope_axes* axes);
+
+/* Fills the table on the host: cosine and sine of h_pos * h_inv_freq, product and functions in binary64, rounded to
+ * float32 once.  Any positions and frequencies: offsets into a longer video, scaled grids, frequencies of any rule.
+ *   h_pos       the F frame, then the Hg height, then the Wg width coordinates
+ *   h_inv_freq  one per pair: (dims[0] + dims[1] + dims[2]) / 2
+ *   h_table     paro_rope_table_floats(s, axes) floats; all pointers are host */
+int paro_rope_table(const paro_shape* s, const paro_rope_axes* axes, const double* h_pos, const double* h_inv_freq,
+                    float* h_table);
+
+/* Rows of d consecutive channels on the device, the row of batch b, head h, token n at element
+ * b * batch + h * head + n * token of `data`: [B,nh,N,d], [B,N,nh,d] or a slice of a fused projection [B,N,3,nh,d].
+ * Every row starts at a multiple of 16 bytes.  Strides are not negative; rows that are written do not overlap
+ * (batch, head and token strides, sorted, each span what the smaller ones cover). */
+typedef struct paro_strided {
+    void* data;
+    int64_t batch, head, token;
+} paro_strided;
+
+/* y = x turned by position; with inverse != 0 turned back, which is also the gradient: dx from dy.  Arithmetic in
+ * binary64, each value rounded once.
+ *   axes, table  as above; table is on the device, 16-byte aligned, and may be NULL where dims are all 0
+ *   x, y         rows of dtype; y may be x (the same pointer and strides) */
+int paro_rope(const paro_shape* s, paro_dtype dtype, const paro_rope_axes* axes, const float* table, int inverse,
+              const paro_strided* x, const paro_strided* y, void* stream);
+
+/* Norm of a head's row x of d channels, entry 0 of each array for Q and 1 for K:
+ *   PARO_NORM_NONE   u = x
+ *   PARO_NORM_RMS    u = x r w,             r = 1 / sqrt(mean(x^2) + eps)
+ *   PARO_NORM_LAYER  u = (x - m) r w + b,   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps)
+ * Weights and biases are float32 [d] on the device, 16-byte aligned, shared by all heads; NULL weights are ones, NULL
+ * biases zeros.  Text tokens take text_weight and text_bias where these are given (joint layers, in which text has
+ * its own projections and norms), else the others.  Weights need a norm, biases PARO_NORM_LAYER. */
+typedef enum paro_norm_kind { PARO_NORM_NONE = 0, PARO_NORM_RMS = 1, PARO_NORM_LAYER = 2 } paro_norm_kind;
+
+typedef struct paro_qk_norm {
+    int32_t kind; /* a paro_norm_kind */
+    double eps;   /* finite, >= 0 (a row of zeros under a norm with eps 0 is NaN, as the formula says) */
+    const float* weight[2];
+    const float* bias[2];
+    const float* text_weight[2];
+    const float* text_bias[2];
+} paro_qk_norm;
+
+/* Where the gradients of a paro_qk_norm go, float32 [d] each (16-byte aligned, overwritten); NULL: not wanted.  A
+ * text_* gradient needs the text_* value itself; without one the text tokens' share is part of the others. */
+typedef struct paro_qk_norm_grad {
+    float* weight[2];
+    float* bias[2];
+    float* text_weight[2];
+    float* text_bias[2];
+} paro_qk_norm_grad;
+
+/* Q and K normalised per head and turned by position in one pass: sums and values in binary64, rounded once to dtype.
+ *   q, k, q_out, k_out  rows of dtype; q_out may be q and k_out may be k (the same pointer and strides) */
+int paro_qk_norm_rope(const paro_shape* s, paro_dtype dtype, const paro_rope_axes* axes, const float* table,
+                      const paro_qk_norm* norm, const paro_strided* q, const paro_strided* k, const paro_strided* q_out,
+                      const paro_strided* k_out, void* stream);
+
+/* Gradients of paro_qk_norm_rope: with g the gradient of an output row turned back, h = x r (or (x - m) r) and
+ * v = g w,  dw = sum g h and db = sum g over batch, heads and tokens, dx = r (v - h mean(v h)) for PARO_NORM_RMS and
+ * r (v - mean(v) - h mean(v h)) for PARO_NORM_LAYER.  Nothing of the forward call is kept: rows are read again.  The
+ * same bits in every call: partial sums meet in a fixed order, in `scratch`.
+ *   q, k                 what the forward call read;  dq_out, dk_out  gradients of its outputs
+ *   dq, dk               receive the gradients of q and k; either may be the dq_out or dk_out, or q or k, that it
+ *                        belongs to (the same pointer and strides)
+ *   grad                 NULL, or where the weights' and biases' gradients go
+ *   scratch              paro_qk_norm_rope_backward_bytes(s) bytes on the device, 16-byte aligned, of any content; may
+ *                        be NULL where no such gradient is wanted.  One call at a time may use it */
+int64_t paro_qk_norm_rope_backward_bytes(const paro_shape* s);
+int paro_qk_norm_rope_backward(const paro_shape* s, paro_dtype dtype, const paro_rope_axes* axes, const float* table,
+                               const paro_qk_norm* norm, const paro_strided* q, const paro_strided* k,
+                               const paro_strided* dq_out, const paro_strided* dk_out, const paro_strided* dq,
+                               const paro_strided* dk, const paro_qk_norm_grad* grad, void* scratch, void* stream);
+
+/* paro_qk_norm_rope to float32 followed by paro_permute_quantize_qkv of its outputs and v, in one launch and without
+ * the intermediate tensors: codes and scales are those of the two calls bit for bit (with float32 v; bfloat16 v is
+ * widened, which is exact).
+ *   q, k, v      rows of dtype, default token order
+ *   (bits_qk, bits_pv), h_perm_ids, *_codes, s*: as paro_permute_quantize_qkv */
+int paro_qk_norm_rope_quantize_qkv(const paro_shape* s, paro_dtype dtype, int bits_qk, int bits_pv, const uint8_t* h_perm_ids,
+                                   const paro_rope_axes* axes, const float* table, const paro_qk_norm* norm,
+                                   const paro_strided* q, const paro_strided* k, const paro_strided* v, void* q_codes, float* sq,
+                                   void* k_codes, float* sk, void* v_codes, float* sv, void* stream);
+
 /* ---- mask prefetch (Sec. 4.2 (1), per-head masks fetched just before use; App. C "Overhead of Prefetch") ----
  * Masks differ per transformer block and timestep, so only the mask of the call at hand lives on
  * the GPU: while attention runs with one block list, the caller copies the next bitmask to the

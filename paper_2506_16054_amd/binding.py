@@ -22,6 +22,11 @@ PARO_F32 = 0
 PARO_BF16 = 1
 PARO_ROWS = 0
 PARO_VT = 1
+PARO_PAIRS_ADJACENT = 0
+PARO_PAIRS_HALVES = 1
+PARO_NORM_NONE = 0
+PARO_NORM_RMS = 1
+PARO_NORM_LAYER = 2
 QKV_BITS = ((8, 8), (8, 4), (4, 4), (4, 8), (16, 16))  # (bits_qk, bits_pv) of the one-launch quantizers and of the attention
 
 LIBPATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libparo.so")
@@ -34,6 +39,8 @@ EXPORTS = (
     "paro_sparse_attn_unpermuted_rawq", "paro_blocklist_cols_device", "paro_permute_quantize_qkv", "paro_permute_quantize_qkv_keep",
     "paro_k_channel_mean", "paro_permute_quantize_smoothed", "paro_permute_quantize_qkv_smoothed", "paro_permute_quantize_kv",
     "paro_calib_row_stats_bytes", "paro_calib_row_stats", "paro_calib_block_stats_from_rows", "paro_calib_metrics_orders", "paro_calib_pick",
+    "paro_rope_table_floats", "paro_rope_table", "paro_rope", "paro_qk_norm_rope", "paro_qk_norm_rope_backward_bytes", "paro_qk_norm_rope_backward",
+    "paro_qk_norm_rope_quantize_qkv",
 )
 
 
@@ -45,6 +52,25 @@ class ParoError(RuntimeError):
 
 class paro_shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "nh", "d", "F", "Hg", "Wg", "T_text", "block")]
+
+
+class paro_rope_axes(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32 * 3), ("pairs", ctypes.c_int32)]
+
+
+class paro_strided(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("batch", "head", "token")]
+
+
+_PairOfVectors = ctypes.c_void_p * 2
+
+
+class paro_qk_norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_double)] + [(n, _PairOfVectors) for n in ("weight", "bias", "text_weight", "text_bias")]
+
+
+class paro_qk_norm_grad(ctypes.Structure):
+    _fields_ = [(n, _PairOfVectors) for n in ("weight", "bias", "text_weight", "text_bias")]
 
 
 _lib = None
@@ -98,6 +124,16 @@ def lib() -> ctypes.CDLL:
         L.paro_permute_quantize_qkv_smoothed.argtypes = [sp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.paro_k_channel_mean.argtypes = [sp, i32, vp, vp, vp]
         L.paro_permute_quantize_smoothed.argtypes = [sp, i32, i32, vp, vp, vp, vp, vp, vp]
+        ap, rp, np_, gp = (ctypes.POINTER(c) for c in (paro_rope_axes, paro_strided, paro_qk_norm, paro_qk_norm_grad))
+        L.paro_rope_table_floats.restype = i64
+        L.paro_rope_table_floats.argtypes = [sp, ap]
+        L.paro_rope_table.argtypes = [sp, ap, vp, vp, vp]
+        L.paro_rope.argtypes = [sp, i32, ap, vp, i32, rp, rp, vp]
+        L.paro_qk_norm_rope.argtypes = [sp, i32, ap, vp, np_, rp, rp, rp, rp, vp]
+        L.paro_qk_norm_rope_backward_bytes.restype = i64
+        L.paro_qk_norm_rope_backward_bytes.argtypes = [sp]
+        L.paro_qk_norm_rope_backward.argtypes = [sp, i32, ap, vp, np_, rp, rp, rp, rp, rp, rp, gp, vp, vp]
+        L.paro_qk_norm_rope_quantize_qkv.argtypes = [sp, i32, i32, i32, vp, ap, vp, np_, rp, rp, rp, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -581,6 +617,174 @@ def paro_calib_mask(s: paro_shape, block_sum, density: float, bitmask) -> None:
     _require(block_sum, "block_sum", (s.B, s.nh, kb, kb), torch.float32)
     _require(bitmask, "bitmask", (s.nh, (kb * kb + 7) // 8), torch.uint8)
     _check(lib().paro_calib_mask(ctypes.byref(s), _ptr(block_sum), float(density), _ptr(bitmask), _stream()))
+
+
+# ---- norms of Q and K, rotation by position -----------------------------------------------------
+def make_rope_axes(dims, pairs: int = PARO_PAIRS_ADJACENT) -> paro_rope_axes:
+    """dims: channels turned by the frame, the height and the width coordinate."""
+    return paro_rope_axes((ctypes.c_int32 * 3)(*dims), pairs)
+
+
+def paro_rope_table_floats(s: paro_shape, axes: paro_rope_axes) -> int:
+    n = lib().paro_rope_table_floats(ctypes.byref(s), ctypes.byref(axes))
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def paro_rope_table(s: paro_shape, axes: paro_rope_axes, pos, inv_freq) -> np.ndarray:
+    """Host: float32 [entries, 2] (cosine, sine).  pos: the F frame, Hg height and Wg width coordinates, one array behind the other or a
+    sequence of three; inv_freq: one frequency per pair, likewise."""
+    flat = lambda x: np.ascontiguousarray(np.concatenate([np.asarray(a, np.float64).reshape(-1) for a in x]) if isinstance(x, (tuple, list)) and
+                                          len(x) and np.ndim(x[0]) else x, np.float64)
+    pos, inv_freq = flat(pos), flat(inv_freq)
+    table = np.empty((paro_rope_table_floats(s, axes) // 2, 2), np.float32)
+    for name, x, n in (("pos", pos, s.F + s.Hg + s.Wg), ("inv_freq", inv_freq, sum(axes.dims) // 2)):
+        if x.shape != (n,):
+            raise ParoError(PARO_EINVAL, "%s has shape %s, expected (%d,)" % (name, x.shape, n))
+    _check(lib().paro_rope_table(ctypes.byref(s), ctypes.byref(axes), pos.ctypes.data, inv_freq.ctypes.data, table.ctypes.data))
+    return table
+
+
+class _Vectors:
+    """What QkNorm and QkNormGrad hold: float32 [d] device tensors or None, in the order of the C structures."""
+    NAMES = tuple("%s%s_%s" % (text, x, kind) for text in ("", "text_") for kind in ("weight", "bias") for x in "qk")
+
+    def __init__(self, **vectors):
+        unknown = set(vectors) - set(self.NAMES)
+        if unknown:
+            raise ParoError(PARO_EINVAL, "unknown vector %s" % sorted(unknown)[0])
+        self.vectors = tuple(vectors.get(name) for name in self.NAMES)
+
+    def _fill(self, struct, d: int, dev: int) -> None:
+        import torch
+
+        for i, (name, t) in enumerate(zip(self.NAMES, self.vectors)):
+            if t is not None:
+                _require(t, name, (d,), torch.float32)
+                _on_device(t, name, dev)
+                getattr(struct, ("weight", "bias", "text_weight", "text_bias")[i // 2])[i % 2] = t.data_ptr()
+
+
+class QkNorm(_Vectors):
+    """The norms of Q and K of a layer: kind and eps, and of q_weight, k_weight, q_bias, k_bias, text_q_weight, text_k_weight,
+    text_q_bias, text_k_bias (float32 [d] device tensors) those the layer has."""
+
+    def __init__(self, kind: int, eps: float = 1e-6, **vectors):
+        super().__init__(**vectors)
+        self.kind, self.eps = int(kind), float(eps)
+
+    def struct(self, d: int, dev: int) -> paro_qk_norm:
+        c = paro_qk_norm(kind=self.kind, eps=self.eps)
+        self._fill(c, d, dev)
+        return c
+
+
+class QkNormGrad(_Vectors):
+    """Where the gradients of a QkNorm go, under the same names; those left out are not computed."""
+
+    def struct(self, d: int, dev: int) -> paro_qk_norm_grad:
+        c = paro_qk_norm_grad()
+        self._fill(c, d, dev)
+        return c
+
+
+def _on_device(t, name: str, dev: int) -> None:
+    if t.get_device() != dev:
+        raise ParoError(PARO_EINVAL, "%s is on device %d, the current one is %d" % (name, t.get_device(), dev))
+
+
+def _strided(t, name: str, shape, dtype, dev: int) -> paro_strided:
+    """Rows of [B, nh, N, d] in any strides but the last, which is 1."""
+    if not t.is_cuda or tuple(t.shape) != shape:
+        raise ParoError(PARO_EINVAL, "%s must be a device tensor of shape %s, not %s" % (name, shape, tuple(t.shape)))
+    if t.dtype != dtype:
+        raise ParoError(PARO_EINVAL, "%s has dtype %s, expected %s" % (name, t.dtype, dtype))
+    if t.stride(3) != 1:
+        raise ParoError(PARO_EINVAL, "%s: the channels of a row must be consecutive" % name)
+    _on_device(t, name, dev)
+    return paro_strided(t.data_ptr(), *t.stride()[:3])
+
+
+def _rotation(s: paro_shape, axes: paro_rope_axes, table, dev: int):
+    """The table's address; None where no channel turns."""
+    import torch
+
+    floats = paro_rope_table_floats(s, axes)
+    if not floats:
+        return None
+    if table is None:
+        raise ParoError(PARO_EINVAL, "table is None")
+    _require(table, "table", (floats // 2, 2), torch.float32)
+    _on_device(table, "table", dev)
+    return _ptr(table)
+
+
+def _current_device(t) -> int:
+    import torch
+
+    if not t.is_cuda:
+        raise ParoError(PARO_EINVAL, "tensors must be on the device")
+    return torch.cuda.current_device()
+
+
+def paro_rope(s: paro_shape, axes: paro_rope_axes, table, x, y, inverse: bool = False) -> None:
+    """x, y: [B, nh, N, d] float32 or bfloat16, any strides of whole 16-byte rows; y may be x.  inverse turns back (the gradient)."""
+    m, dev = _dims(s), _current_device(x)
+    r = [_strided(t, name, m.x, x.dtype, dev) for name, t in (("x", x), ("y", y))]
+    _check(lib().paro_rope(ctypes.byref(s), _dtype_code(x), ctypes.byref(axes), _rotation(s, axes, table, dev), int(bool(inverse)), *map(ctypes.byref, r),
+                           _stream()))
+
+
+def paro_qk_norm_rope(s: paro_shape, axes: paro_rope_axes, table, norm: QkNorm, q, k, q_out, k_out) -> None:
+    m, dev = _dims(s), _current_device(q)
+    r = [_strided(t, name, m.x, q.dtype, dev) for name, t in (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out))]
+    _check(lib().paro_qk_norm_rope(ctypes.byref(s), _dtype_code(q), ctypes.byref(axes), _rotation(s, axes, table, dev),
+                                   ctypes.byref(norm.struct(s.d, dev)), *map(ctypes.byref, r), _stream()))
+
+
+def paro_qk_norm_rope_backward_bytes(s: paro_shape) -> int:
+    n = lib().paro_qk_norm_rope_backward_bytes(ctypes.byref(s))
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def paro_qk_norm_rope_backward(s: paro_shape, axes: paro_rope_axes, table, norm: QkNorm, q, k, dq_out, dk_out, dq, dk,
+                               grad: Optional[QkNormGrad] = None, scratch=None) -> None:
+    """dq_out, dk_out: gradients of the outputs; dq, dk receive those of q and k, `grad` those of the norms.  scratch: uint8
+    [paro_qk_norm_rope_backward_bytes(s)], needed where grad holds a vector."""
+    import torch
+
+    m, dev = _dims(s), _current_device(q)
+    r = [_strided(t, name, m.x, q.dtype, dev)
+         for name, t in (("q", q), ("k", k), ("dq_out", dq_out), ("dk_out", dk_out), ("dq", dq), ("dk", dk))]
+    if scratch is not None:
+        _require(scratch, "scratch", (paro_qk_norm_rope_backward_bytes(s),), torch.uint8)
+        _on_device(scratch, "scratch", dev)
+    g = None if grad is None else grad.struct(s.d, dev)
+    _check(lib().paro_qk_norm_rope_backward(ctypes.byref(s), _dtype_code(q), ctypes.byref(axes), _rotation(s, axes, table, dev),
+                                            ctypes.byref(norm.struct(s.d, dev)), *map(ctypes.byref, r), None if g is None else ctypes.byref(g),
+                                            _ptr(scratch), _stream()))
+
+
+def paro_qk_norm_rope_quantize_qkv(s: paro_shape, bits_qk: int, bits_pv: int, perm_ids, axes: paro_rope_axes, table, norm: QkNorm, q, k, v,
+                                   q_codes, sq, k_codes, sk, v_codes, sv) -> None:
+    """paro_qk_norm_rope and paro_permute_quantize_qkv in one launch; q, k, v: [B, nh, N, d], any strides of whole 16-byte rows."""
+    import torch
+
+    m, dev = _dims(s), _current_device(q)
+    r = [_strided(t, name, m.x, q.dtype, dev) for name, t in (("q", q), ("k", k), ("v", v))]
+    rows, ct_qk = m.rows4 if bits_qk == 4 else m.rows, torch.bfloat16 if bits_qk == 16 else torch.int8
+    for name, t, shape, dtype in (("q_codes", q_codes, rows, ct_qk), ("k_codes", k_codes, rows, ct_qk),
+                                  ("v_codes", v_codes, m.vt4 if bits_pv == 4 else m.vt, torch.bfloat16 if bits_pv == 16 else torch.int8),
+                                  ("sq", sq, m.scales, torch.float32), ("sk", sk, m.scales, torch.float32), ("sv", sv, m.scales, torch.float32)):
+        _require(t, name, shape, dtype)
+        _on_device(t, name, dev)
+    p = _perm_bytes(s, perm_ids)
+    _check(lib().paro_qk_norm_rope_quantize_qkv(ctypes.byref(s), _dtype_code(q), int(bits_qk), int(bits_pv), p, ctypes.byref(axes),
+                                                _rotation(s, axes, table, dev), ctypes.byref(norm.struct(s.d, dev)), *map(ctypes.byref, r),
+                                                _ptr(q_codes), _ptr(sq), _ptr(k_codes), _ptr(sk), _ptr(v_codes), _ptr(sv), _stream()))
 
 
 def _attn_operands(s: paro_shape, bits_qk: int, bits_pv: int, q, sq, k, sk, v, sv, row_ptr, col_idx) -> None:

@@ -23,7 +23,7 @@ LIBDIR = os.path.join(PKG, "lib")
 LIBPATH = os.path.join(LIBDIR, "libparo.so")
 PROBE_LIBPATH = os.path.join(LIBDIR, "libparo_probe.so")
 TIMELINE_LIBNAME = "libparo_timeline.so"
-SOURCES = ("host_api.cpp", "permute.hip", "quantize.hip", "blocklist.hip", "calibrate.hip", "sparse_attn.hip")
+SOURCES = ("host_api.cpp", "permute.hip", "quantize.hip", "norm_rope.hip", "blocklist.hip", "calibrate.hip", "sparse_attn.hip")
 FASTCALL_LIBNAME = "paro_fastcall.so"
 PROBE_SOURCES = ("probe/issue_probe.hip",)
 

@@ -14,6 +14,9 @@ int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)))
 // Shape check shared by every entry point; fills N, k on success.
 int check_shape(const paro_shape* s, int64_t* n_tokens, int64_t* k_blocks);
 
+// Channels that turn with the position: even, not negative, together no more than a row has.
+int check_axes(const paro_shape* s, const paro_rope_axes* axes);
+
 int check_launch(const char* what);
 
 constexpr int kMaxHeads = 256;

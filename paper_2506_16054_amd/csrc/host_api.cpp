@@ -1,5 +1,6 @@
 // Host-only part of libparo: status text, shape arithmetic, the gather index of an axis order
 // (paper Sec. 4.1), the PARO_VT slot map and the bitmask -> block-list conversion (Sec. 4.2).
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -38,6 +39,18 @@ int check_shape(const paro_shape* s, int64_t* n_tokens, int64_t* k_blocks) {
         return fail(PARO_EUNSUPPORTED, "B*nh*k=%lld exceeds the launch limit", (long long)((int64_t)s->B * s->nh * k));
     if (n_tokens) *n_tokens = n;
     if (k_blocks) *k_blocks = k;
+    return PARO_OK;
+}
+
+int check_axes(const paro_shape* s, const paro_rope_axes* axes) {
+    if (!axes) return fail(PARO_EINVAL, "axes is NULL");
+    if (axes->pairs != PARO_PAIRS_ADJACENT && axes->pairs != PARO_PAIRS_HALVES) return fail(PARO_EINVAL, "pairs=%d is not a paro_pairs", (int)axes->pairs);
+    int64_t channels = 0;
+    for (int a = 0; a < 3; ++a) {
+        if (axes->dims[a] < 0 || axes->dims[a] % 2) return fail(PARO_EINVAL, "dims[%d]=%d must be even and >= 0", a, (int)axes->dims[a]);
+        channels += axes->dims[a];
+    }
+    if (channels > s->d) return fail(PARO_EINVAL, "dims are %lld channels together, more than d=%d", (long long)channels, (int)s->d);
     return PARO_OK;
 }
 
@@ -125,6 +138,31 @@ int paro_perm_index(const paro_shape* s, int perm_id, int32_t* h_idx) {
             for (int c2 = 0; c2 < dims[o.a[2]]; ++c2)
                 h_idx[pos++] = c0 * stride[o.a[0]] + c1 * stride[o.a[1]] + c2 * stride[o.a[2]];
     for (; pos < n; ++pos) h_idx[pos] = (int32_t)pos;  // text tokens keep their place
+    return PARO_OK;
+}
+
+int64_t paro_rope_table_floats(const paro_shape* s, const paro_rope_axes* axes) {
+    if (int st = check_shape(s, nullptr, nullptr)) return st;
+    if (int st = check_axes(s, axes)) return st;
+    return (int64_t)axes->dims[0] * s->F + (int64_t)axes->dims[1] * s->Hg + (int64_t)axes->dims[2] * s->Wg;
+}
+
+int paro_rope_table(const paro_shape* s, const paro_rope_axes* axes, const double* h_pos, const double* h_inv_freq, float* h_table) {
+    const int64_t floats = paro_rope_table_floats(s, axes);
+    if (floats < 0) return (int)floats;
+    if (floats && (!h_pos || !h_inv_freq || !h_table)) return fail(PARO_EINVAL, "h_pos, h_inv_freq and h_table must not be NULL");
+    const int extent[3] = {s->F, s->Hg, s->Wg};
+    for (int a = 0; a < 3; ++a) {
+        const int pairs = axes->dims[a] / 2;
+        for (int i = 0; i < extent[a]; ++i)
+            for (int p = 0; p < pairs; ++p) {
+                const double angle = h_pos[i] * h_inv_freq[p];
+                *h_table++ = (float)cos(angle);
+                *h_table++ = (float)sin(angle);
+            }
+        h_pos += extent[a];
+        h_inv_freq += pairs;
+    }
     return PARO_OK;
 }
 

@@ -110,6 +110,18 @@ class ParoAttention:
         self.prepare_fused(q, k, v)
         return self.attend_fused()
 
+    # ---- Q and K as their projections leave them: norms, rotation, reorder and quantizer in one launch
+    def prepare_norm_rope(self, step: "QkNormRope", q, k, v) -> None:
+        """prepare_fused_qkv of step.forward(q, k) and v, without the normalised and rotated tensors; q, k, v may be slices of one
+        projection's output."""
+        fq, fk = self._fused_buffers()
+        pb.paro_qk_norm_rope_quantize_qkv(self.s, self.bits_qk, self.bits_pv, self.perm_ids, step.axes, step.table, step.norm, q, k, v, fq, self.sq,
+                                          fk, self.sk, self.vc, self.sv)
+
+    def run_norm_rope(self, step: "QkNormRope", q, k, v):
+        self.prepare_norm_rope(step, q, k, v)
+        return self.attend_fused()
+
     # ---- optional pre-conditioning of K: the per-channel mean over the tokens is removed in the quantizer's loads
     def prepare_fused_smooth_k(self, q, k, v) -> None:
         """prepare_fused with the channel mean of K removed (integer K codes only): two launches."""
@@ -153,6 +165,44 @@ class ParoAttention:
     def run_rawq(self, q, k, v):
         self.prepare_kv(k, v)
         return self.attend_rawq(q)
+
+
+class QkNormRope:
+    """The step between the projections of Q and K and the attention call, for one layer: norm per head and rotation by the token's
+    (frame, height, width) position.  Owns the table of angles.
+
+    dims      channels turned by the frame, height and width coordinate (even, together at most d)
+    norm      pb.QkNorm; None: rotation alone
+    pos       the three axes' coordinates, default 0, 1, 2, ..
+    inv_freq  the three axes' frequencies, default theta ** (-2 j / dims[a]) for the j-th pair of an axis"""
+
+    def __init__(self, shape: pb.paro_shape, dims, pairs: int = pb.PARO_PAIRS_ADJACENT, norm=None, pos=None, inv_freq=None, theta: float = 10000.0,
+                 device="cuda:0"):
+        self.s = shape
+        self.axes = pb.make_rope_axes(dims, pairs)
+        self.norm = pb.QkNorm(pb.PARO_NORM_NONE) if norm is None else norm
+        if pos is None:
+            pos = [np.arange(n, dtype=np.float64) for n in (shape.F, shape.Hg, shape.Wg)]
+        if inv_freq is None:
+            inv_freq = [theta ** (-np.arange(0, dim, 2, dtype=np.float64) / dim) if dim else np.empty(0) for dim in dims]
+        self.h_table = pb.paro_rope_table(shape, self.axes, pos, inv_freq)
+        self.table = torch.from_numpy(self.h_table).to(device)
+
+    def forward(self, q, k, q_out=None, k_out=None):
+        """Q and K [B, nh, N, d] (any strides of whole rows) normalised and rotated; in new tensors unless told where."""
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        pb.paro_qk_norm_rope(self.s, self.axes, self.table, self.norm, q, k, q_out, k_out)
+        return q_out, k_out
+
+    def backward(self, q, k, dq_out, dk_out, grad=None, dq=None, dk=None, scratch=None):
+        """The gradients of q and k from those of forward's outputs; the norms' go where `grad` (pb.QkNormGrad) says."""
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+        if scratch is None and grad is not None:
+            scratch = torch.empty((pb.paro_qk_norm_rope_backward_bytes(self.s),), dtype=torch.uint8, device=q.device)
+        pb.paro_qk_norm_rope_backward(self.s, self.axes, self.table, self.norm, q, k, dq_out, dk_out, dq, dk, grad, scratch)
+        return dq, dk
 
 
 class MaskPrefetcher:
