@@ -1,9 +1,9 @@
 // Norms of Q and K per head and their rotation by the token's (frame, height, width) position: forward, gradients, and both
 // with the reorder (paper Sec. 4.1) and the block quantizer (Sec. 4.3 (1)) behind them.
 //
-// A row is the d channels of one token of one head.  d / 16 lanes share it, 16 channels each: eight from the front half of the
-// row (8 L ..) and the eight that lie d / 2 behind them, so that both ways to pair channels find their pairs inside a lane.
-// Row sums meet in two or three steps across neighbouring lanes (DPP); nothing goes through LDS.
+// A row is the d channels of one token of one head.  d / 8 lanes share it, eight channels each: for adjacent pairs the eight
+// from 8 L on, for pairs across the halves four from 4 L on and the four that lie d / 2 behind them, so that a lane holds both
+// channels of its pairs 4 L .. 4 L + 3.  Row sums meet across neighbouring lanes (DPP); nothing goes through LDS.
 //
 // The angles' table separates by axis: some KB instead of some MB per layer, so it comes from the caches nearest to the compute
 // unit.
@@ -14,6 +14,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "quantize_tile.h"
 
@@ -23,21 +24,20 @@ constexpr int kThreads = 256;
 
 // Channels turned by position: what the kernels need of a paro_rope_axes, its table and the grid.
 struct Turning {
-    const float2* table;
+    const float* table;
     int pairs[3];  // pairs per axis
     int base[3];   // first entry of an axis in the table
     int total;     // pairs that turn; pair p turns with the axis whose run of pairs holds it
+    bool fours;    // every axis has a multiple of four pairs: four consecutive entries from a multiple of four on are one axis' and 32 aligned bytes
     int n_img, Hg, Wg;
     double inv_hg, inv_wg;
     float sign;  // -1: turned back
-    int halves;
 };
 
 // Norms: entry [tensor][text].
 struct Norms {
     const float* w[2][2];
     const float* b[2][2];
-    int kind;
     double eps;
 };
 
@@ -52,65 +52,74 @@ struct Rows {
 // or more from the next integers, and is off by less than 2^-51 n / divisor.
 __device__ inline int quotient_of(int n, double inv) { return (int)(((double)n + 0.5) * inv); }
 
-// ---- the 16 channels of a lane -------------------------------------------------------------------------------------
-// As loaded: 8 channels are 16 bytes of bf16 or 32 of binary32.
-template <typename T>
-struct LaneRow {
-    static constexpr int Q = sizeof(T) / 2;  // 16-byte pieces per 8 channels
-    uint4 q[2 * Q];
-    template <int D>
-    __device__ __forceinline__ void load(const T* row, int L) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int i = 0; i < Q; ++i) q[half * Q + i] = ((const uint4*)(row + half * (D / 2) + 8 * L))[i];
-    }
-    __device__ __forceinline__ float operator[](int e) const {
-        if constexpr (sizeof(T) == 2) {
-            const uint4& v = q[e >> 3];
-            const unsigned w = (e & 7) < 2 ? v.x : (e & 7) < 4 ? v.y : (e & 7) < 6 ? v.z : v.w;
-            return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
-        } else {
-            const uint4& v = q[e >> 2];
-            return __uint_as_float((e & 3) == 0 ? v.x : (e & 3) == 1 ? v.y : (e & 3) == 2 ? v.z : v.w);
-        }
-    }
-};
-
+// ---- the 8 channels of a lane --------------------------------------------------------------------------------------
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+typedef unsigned uint2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ inline unsigned pack_bf16(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector((float2v){a, b}, bf16x2)); }
 
-template <int D>
-__device__ __forceinline__ void store_lane(uint16_t* row, int L, const float (&y)[16]) {
+// As in memory: 16 bytes of bf16 or 32 of binary32, in one piece or in two (HALVES).
+template <typename T, int D, bool HALVES>
+struct LaneRow {
+    static constexpr int WORDS = 2 * sizeof(T);
+    unsigned w[WORDS];
+    // where the lane's second four channels lie behind its first
+    static constexpr int SECOND = HALVES ? D / 2 : 4;
+    static __device__ __forceinline__ int first(int L) { return HALVES ? 4 * L : 8 * L; }
+
+    __device__ __forceinline__ void load(const T* row, int L) {
+        const T* p = row + first(L);
+        if constexpr (sizeof(T) == 2 && !HALVES) {
+            const uint4v v = *(const uint4v*)p;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const float* v = y + 8 * half;
-        *(uint4*)(row + half * (D / 2) + 8 * L) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    }
-}
-template <int D>
-__device__ __forceinline__ void store_lane(float* row, int L, const float (&y)[16]) {
+            for (int i = 0; i < 4; ++i) w[i] = v[i];
+        } else {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        float4* out = (float4*)(row + half * (D / 2) + 8 * L);
-        const float* v = y + 8 * half;
-        out[0] = make_float4(v[0], v[1], v[2], v[3]);
-        out[1] = make_float4(v[4], v[5], v[6], v[7]);
+            for (int half = 0; half < 2; ++half) {
+                if constexpr (sizeof(T) == 2) {
+                    const uint2v v = *(const uint2v*)(p + half * SECOND);
+                    w[2 * half] = v[0], w[2 * half + 1] = v[1];
+                } else {
+                    const uint4v v = *(const uint4v*)(p + half * SECOND);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[4 * half + i] = v[i];
+                }
+            }
+        }
     }
-}
+    __device__ __forceinline__ float operator[](int e) const {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        else return __uint_as_float(w[e]);
+    }
+    static __device__ __forceinline__ void store(T* row, int L, const float (&y)[8]) {
+        T* p = row + first(L);
+        if constexpr (sizeof(T) == 2) {
+            const unsigned v[4] = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+            if constexpr (HALVES) {
+                *(uint2v*)p = (uint2v){v[0], v[1]};
+                *(uint2v*)(p + SECOND) = (uint2v){v[2], v[3]};
+            } else {
+                *(uint4v*)p = (uint4v){v[0], v[1], v[2], v[3]};
+            }
+        } else {
+            ((float4*)p)[0] = make_float4(y[0], y[1], y[2], y[3]);
+            *(float4*)(p + SECOND) = make_float4(y[4], y[5], y[6], y[7]);
+        }
+    }
+};
 
 // A lane's channels of a float32 [d] vector, or `other` where there is none.
-template <int D>
-__device__ __forceinline__ void load_vector(const float* v, int L, float other, float (&x)[16]) {
+template <int D, bool HALVES>
+__device__ __forceinline__ void load_vector(const float* v, int L, float other, float (&x)[8]) {
     if (v) {
-        LaneRow<float> r;
-        r.load<D>(v, L);
+        LaneRow<float, D, HALVES> r;
+        r.load(v, L);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = r[e];
+        for (int e = 0; e < 8; ++e) x[e] = r[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = other;
+        for (int e = 0; e < 8; ++e) x[e] = other;
     }
 }
 
@@ -121,13 +130,14 @@ template <int CTRL>
 __device__ __forceinline__ double moved(double v) { return __hiloint2double(moved<CTRL>(__double2hiint(v)), moved<CTRL>(__double2loint(v))); }
 template <int CTRL>
 __device__ __forceinline__ float moved(float v) { return __int_as_float(moved<CTRL>(__float_as_int(v))); }
-// Sum over the D / 16 neighbouring lanes of a row, in every one of them: the lane beside (quad_perm 1 0 3 2), the pair beside
-// (2 3 0 1), the other four of eight (row_half_mirror).
+// Sum over the D / 8 neighbouring lanes of a row, in every one of them: the lane beside (quad_perm 1 0 3 2), the pair beside
+// (2 3 0 1), the other four of eight (row_half_mirror), the other eight of sixteen (row_mirror).
 template <int D, typename V>
 __device__ __forceinline__ V row_sum(V v) {
     v += moved<0xB1>(v);
     v += moved<0x4E>(v);
-    if constexpr (D == 128) v += moved<0x141>(v);
+    v += moved<0x141>(v);
+    if constexpr (D == 128) v += moved<0x140>(v);
     return v;
 }
 
@@ -142,18 +152,18 @@ __device__ __forceinline__ double rsqrt_of(double v) {
 }
 
 // What a row is normalised by: value e becomes (x[e] - mean) r.
-template <int D, typename T>
-__device__ __forceinline__ void row_norm(const LaneRow<T>& x, int kind, double eps, double& mean, double& r) {
+template <int KIND, typename T, int D, bool HALVES>
+__device__ __forceinline__ void row_norm(const LaneRow<T, D, HALVES>& x, double eps, double& mean, double& r) {
     mean = 0.0;
-    if (kind == PARO_NORM_LAYER) {
+    if constexpr (KIND == PARO_NORM_LAYER) {
         double s = 0.0;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s += (double)x[e];
+        for (int e = 0; e < 8; ++e) s += (double)x[e];
         mean = row_sum<D>(s) * (1.0 / D);
     }
     double s = 0.0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < 8; ++e) {
         const double v = (double)x[e] - mean;
         s = fma(v, v, s);
     }
@@ -161,88 +171,84 @@ __device__ __forceinline__ void row_norm(const LaneRow<T>& x, int kind, double e
 }
 
 // ---- turning -------------------------------------------------------------------------------------------------------
-// Pair e of a lane: channels (2e, 2e + 1) of its 16 (PARO_PAIRS_ADJACENT) or (e, 8 + e) (PARO_PAIRS_HALVES).  Pairs 0 .. 3 and 4 .. 7
-// are four consecutive pairs of the row each.
+// Pair e of a lane: its channels (2e, 2e + 1), or (e, 4 + e) with HALVES.
 struct LaneTurn {
-    float c[8], s[8];
+    float c[4], s[4];
     unsigned turned;  // bit e: pair e turns
+    __device__ __forceinline__ void none() {
+        turned = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = 1.0f, s[e] = 0.0f;
+    }
 };
 
-template <int D>
-__device__ __forceinline__ LaneTurn load_turn(const Turning& t, int L, int f, int h, int w) {
-    LaneTurn r;
-    r.turned = 0;
-    const int e0 = t.base[0] + f * t.pairs[0], e1 = t.base[1] + h * t.pairs[1] - t.pairs[0], e2 = t.base[2] + w * t.pairs[2] - t.pairs[0] - t.pairs[1];
-    const int to1 = t.pairs[0], to2 = t.pairs[0] + t.pairs[1];
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-        const int p0 = t.halves ? 8 * L + 4 * g : g * (D / 4) + 4 * L;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int p = p0 + i, e = 4 * g + i;
-            r.c[e] = 1.0f;
-            r.s[e] = 0.0f;
-            if (p < t.total) {
-                const float2 v = t.table[(p < to1 ? e0 : p < to2 ? e1 : e2) + p];
-                r.c[e] = v.x;
-                r.s[e] = v.y * t.sign;
-                r.turned |= 1u << e;
-            }
-        }
+__device__ __forceinline__ void load_turn(const Turning& t, int L, int f, int h, int w, LaneTurn& r) {
+    const int to1 = t.pairs[0], to2 = t.pairs[0] + t.pairs[1], p0 = 4 * L;
+    const int e0 = t.base[0] + f * t.pairs[0], e1 = t.base[1] + h * t.pairs[1] - to1, e2 = t.base[2] + w * t.pairs[2] - to2;
+    r.none();
+    if (t.fours) {
+        if (p0 >= t.total) return;
+        const float4* v = (const float4*)(t.table + 2 * (int64_t)((p0 < to1 ? e0 : p0 < to2 ? e1 : e2) + p0));
+        const float4 a = v[0], b = v[1];
+        r.c[0] = a.x, r.c[1] = a.z, r.c[2] = b.x, r.c[3] = b.z;
+        r.s[0] = a.y * t.sign, r.s[1] = a.w * t.sign, r.s[2] = b.y * t.sign, r.s[3] = b.w * t.sign;
+        r.turned = 15;
+        return;
     }
-    return r;
-}
-
-// One pair: values that do not turn stay as they are, whatever their partner holds.
-template <typename V>
-__device__ __forceinline__ void turn(V& x, V& y, float c, float s, bool turned) {
-    const V a = fma(x, (V)c, -(y * (V)s)), b = fma(x, (V)s, y * (V)c);
-    x = turned ? a : x;
-    y = turned ? b : y;
-}
-
-template <typename V>
-__device__ __forceinline__ void turn_lane(V (&u)[16], const LaneTurn& t, int halves) {
-    if (halves) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) turn(u[e], u[8 + e], t.c[e], t.s[e], t.turned >> e & 1);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) turn(u[2 * e], u[2 * e + 1], t.c[e], t.s[e], t.turned >> e & 1);
+    for (int e = 0; e < 4; ++e) {
+        const int p = p0 + e;
+        if (p < t.total) {
+            const float2 v = *(const float2*)(t.table + 2 * (int64_t)((p < to1 ? e0 : p < to2 ? e1 : e2) + p));
+            r.c[e] = v.x;
+            r.s[e] = v.y * t.sign;
+            r.turned |= 1u << e;
+        }
     }
 }
 
 // Grid coordinates of a token in default order; text tokens do not turn.
-template <int D>
-__device__ __forceinline__ LaneTurn turn_of_token(const Turning& t, int L, int n) {
-    if (n >= t.n_img || t.total == 0) {
-        LaneTurn r;
-        r.turned = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r.c[e] = 1.0f, r.s[e] = 0.0f;
-        return r;
+__device__ __forceinline__ void turn_of_token(const Turning& t, int L, int n, LaneTurn& r) {
+    if (n < t.n_img && t.total) {
+        const int q = quotient_of(n, t.inv_wg), f = quotient_of(q, t.inv_hg);
+        load_turn(t, L, f, q - f * t.Hg, n - q * t.Wg, r);
+    } else {
+        r.none();
     }
-    const int q = quotient_of(n, t.inv_wg), f = quotient_of(q, t.inv_hg);
-    return load_turn<D>(t, L, f, q - f * t.Hg, n - q * t.Wg);
+}
+
+// A value that does not turn stays as it is, whatever its partner holds; a wavefront whose pairs all turn needs no selection.
+template <bool HALVES, typename V>
+__device__ __forceinline__ void turn_lane(V (&u)[8], const LaneTurn& t) {
+    const bool all = __all(t.turned == 15);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        V &x = HALVES ? u[e] : u[2 * e], &y = HALVES ? u[4 + e] : u[2 * e + 1];
+        const V c = t.c[e], s = t.s[e], a = fma(x, c, -(y * s)), b = fma(x, s, y * c);
+        if (all || (t.turned >> e & 1)) x = a, y = b;
+    }
 }
 
 // The row behind norm and rotation, rounded to binary32.
-template <int D, bool NORM, typename T>
-__device__ __forceinline__ void normed_and_turned(const LaneRow<T>& x, const Norms& norm, const float (&w)[16], const float (&b)[16], const LaneTurn& t,
-                                                  int halves, float (&y)[16]) {
-    double u[16];
-    if constexpr (NORM) {
-        double mean, r;
-        row_norm<D>(x, norm.kind, norm.eps, mean, r);
+template <int KIND, typename T, int D, bool HALVES>
+__device__ __forceinline__ void normed_and_turned(const LaneRow<T, D, HALVES>& x, double eps, const float (&w)[8], const float (&b)[8], const LaneTurn& t,
+                                                  float (&y)[8]) {
+    double u[8];
+    if constexpr (KIND == PARO_NORM_NONE) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = fma(((double)x[e] - mean) * r, (double)w[e], (double)b[e]);
+        for (int e = 0; e < 8; ++e) u[e] = (double)x[e];
     } else {
+        double mean, r;
+        row_norm<KIND>(x, eps, mean, r);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] = (double)x[e];
+        for (int e = 0; e < 8; ++e) {
+            const double v = ((double)x[e] - mean) * r;
+            u[e] = KIND == PARO_NORM_LAYER ? fma(v, (double)w[e], (double)b[e]) : v * (double)w[e];
+        }
     }
-    turn_lane(u, t, halves);
+    turn_lane<HALVES>(u, t);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) y[e] = (float)u[e];
+    for (int e = 0; e < 8; ++e) y[e] = (float)u[e];
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------
@@ -254,27 +260,27 @@ struct RowsArgs {
 };
 
 // grid: (token tiles, batches x groups of heads, tensors).  A lane keeps its token's angles and its channels' weights while it goes
-// through the heads.
-template <typename T, int D, bool NORM>
+// through the heads, and reads a row while it works on the one before.
+template <typename T, int D, int KIND, bool HALVES>
 __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(RowsArgs<T> a, Turning t, Norms norm) {
-    constexpr int LANES = D / 16, TOKENS = kThreads / LANES;
+    constexpr int LANES = D / 8, TOKENS = kThreads / LANES;
     const int L = threadIdx.x % LANES, n = blockIdx.x * TOKENS + threadIdx.x / LANES, z = blockIdx.z;
     if (n >= a.n_tokens) return;
     const int groups = (a.nh + a.heads - 1) / a.heads, b = blockIdx.y / groups, h0 = (blockIdx.y - b * groups) * a.heads;
     const int h1 = min(h0 + a.heads, a.nh);
-    const LaneTurn angles = turn_of_token<D>(t, L, n);
-    float w[16], bias[16];
-    if constexpr (NORM) {
-        const int text = n >= t.n_img;
-        load_vector<D>(norm.w[z][text], L, 1.0f, w);
-        load_vector<D>(norm.b[z][text], L, 0.0f, bias);
-    }
+    LaneRow<T, D, HALVES> next;
+    next.load(a.in[z].row(b, h0, n), L);
+    LaneTurn angles;
+    turn_of_token(t, L, n, angles);
+    float w[8], bias[8];
+    if constexpr (KIND != PARO_NORM_NONE) load_vector<D, HALVES>(norm.w[z][n >= t.n_img], L, 1.0f, w);
+    if constexpr (KIND == PARO_NORM_LAYER) load_vector<D, HALVES>(norm.b[z][n >= t.n_img], L, 0.0f, bias);
     for (int h = h0; h < h1; ++h) {
-        LaneRow<T> x;
-        x.template load<D>(a.in[z].row(b, h, n), L);
-        float y[16];
-        normed_and_turned<D, NORM>(x, norm, w, bias, angles, t.halves, y);
-        store_lane<D>(a.out[z].row(b, h, n), L, y);
+        const LaneRow<T, D, HALVES> x = next;
+        if (h + 1 < h1) next.load(a.in[z].row(b, h + 1, n), L);
+        float y[8];
+        normed_and_turned<KIND>(x, norm.eps, w, bias, angles, y);
+        LaneRow<T, D, HALVES>::store(a.out[z].row(b, h, n), L, y);
     }
 }
 
@@ -289,40 +295,46 @@ struct GradArgs {
 
 // grid: (tiles of image tokens, then of text tokens; batches x groups of heads; tensors).  A tile holds tokens of one kind, so a
 // workgroup's sums belong to one set of weights.
-template <typename T, int D>
+template <typename T, int D, int KIND, bool HALVES>
 __global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(GradArgs<T> a, Turning t, Norms norm) {
-    constexpr int LANES = D / 16, TOKENS = kThreads / LANES;
+    constexpr int LANES = D / 8, TOKENS = kThreads / LANES;
+    typedef LaneRow<T, D, HALVES> Lane;
     const int L = threadIdx.x % LANES, row = threadIdx.x / LANES, z = blockIdx.z;
     const int text = (int)blockIdx.x >= a.img_tiles;
     const int n = text ? t.n_img + ((int)blockIdx.x - a.img_tiles) * TOKENS + row : blockIdx.x * TOKENS + row;
     const bool live = n < (text ? a.n_tokens : t.n_img);
     const int groups = (a.nh + a.heads - 1) / a.heads, b = blockIdx.y / groups, h0 = (blockIdx.y - b * groups) * a.heads;
     const int h1 = min(h0 + a.heads, a.nh);
-    float dw[16], db[16];
+    float dw[8], db[8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dw[e] = db[e] = 0.0f;
+    for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.0f;
     if (live) {
-        const LaneTurn angles = turn_of_token<D>(t, L, n);
-        float w[16];
-        load_vector<D>(norm.w[z][text], L, 1.0f, w);
+        Lane next_x, next_dy;
+        next_x.load(a.x[z].row(b, h0, n), L);
+        next_dy.load(a.dy[z].row(b, h0, n), L);
+        LaneTurn angles;
+        turn_of_token(t, L, n, angles);
+        float w[8];
+        load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
         for (int h = h0; h < h1; ++h) {
-            LaneRow<T> x, dy;
-            x.template load<D>(a.x[z].row(b, h, n), L);
-            dy.template load<D>(a.dy[z].row(b, h, n), L);
-            float g[16];
+            const Lane x = next_x, dy = next_dy;
+            if (h + 1 < h1) {
+                next_x.load(a.x[z].row(b, h + 1, n), L);
+                next_dy.load(a.dy[z].row(b, h + 1, n), L);
+            }
+            float g[8], dx[8];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) g[e] = dy[e];
-            turn_lane(g, angles, t.halves);
-            float dx[16];
-            if (norm.kind == PARO_NORM_NONE) {
+            for (int e = 0; e < 8; ++e) g[e] = dy[e];
+            turn_lane<HALVES>(g, angles);
+            if constexpr (KIND == PARO_NORM_NONE) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dx[e] = g[e];
+                for (int e = 0; e < 8; ++e) dx[e] = g[e];
             } else {
                 double mean, r;
-                row_norm<D>(x, norm.kind, norm.eps, mean, r);
-                float xhat[16], mv = 0.0f, mvh = 0.0f;
+                row_norm<KIND>(x, norm.eps, mean, r);
+                float xhat[8], mv = 0.0f, mvh = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
+                for (int e = 0; e < 8; ++e) {
                     xhat[e] = (float)(((double)x[e] - mean) * r);
                     dw[e] = fmaf(g[e], xhat[e], dw[e]);
                     db[e] += g[e];
@@ -330,25 +342,25 @@ __global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(GradArgs<T> a,
                     mv += v;
                     mvh = fmaf(v, xhat[e], mvh);
                 }
-                mv = norm.kind == PARO_NORM_LAYER ? row_sum<D>(mv) * (1.0f / D) : 0.0f;
+                mv = KIND == PARO_NORM_LAYER ? row_sum<D>(mv) * (1.0f / D) : 0.0f;
                 mvh = row_sum<D>(mvh) * (1.0f / D);
                 const float rf = (float)r;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dx[e] = rf * (fmaf(g[e], w[e], -mv) - xhat[e] * mvh);
+                for (int e = 0; e < 8; ++e) dx[e] = rf * (fmaf(g[e], w[e], -mv) - xhat[e] * mvh);
             }
-            store_lane<D>(a.dx[z].row(b, h, n), L, dx);
+            Lane::store(a.dx[z].row(b, h, n), L, dx);
         }
     }
-    if (!a.partial) return;
-    // the workgroup's sums: [weight, bias][channel][token row], one row more against bank conflicts
+    if (KIND == PARO_NORM_NONE || !a.partial) return;
+    // the workgroup's sums: [channel][token row], one row more against bank conflicts
     __shared__ float meet[D][TOKENS + 1];
     const size_t slot = (size_t)blockIdx.x * gridDim.y + blockIdx.y, slots = (size_t)gridDim.x * gridDim.y;
     float* out = a.partial + (z * slots + slot) * (2 * D);
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
+    for (int kind = 0; kind < (KIND == PARO_NORM_LAYER ? 2 : 1); ++kind) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) meet[(e >> 3) * (D / 2) + 8 * L + (e & 7)][row] = kind ? db[e] : dw[e];
+        for (int e = 0; e < 8; ++e) meet[Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)][row] = kind ? db[e] : dw[e];
         __syncthreads();
         if (threadIdx.x < D) {
             double s = 0.0;
@@ -386,7 +398,7 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(const float* __restrict
 
 // ---- codes of a tile in registers ----------------------------------------------------------------------------------
 // Rows of the staged transposed tile (one channel each) are 4 bytes longer than the block for the integer codes, so that the
-// byte stores of the 8 lanes that hold one token's 64 channels fall into different LDS banks; bf16 takes 16-bit words.
+// byte stores of lanes that hold one token's channels fall into different LDS banks; bf16 takes 16-bit words.
 template <int BITS, int BLK>
 constexpr int stage_row() { return BITS == 16 ? BLK : BLK + 4; }
 template <int BITS, int BLK, int D>
@@ -402,49 +414,65 @@ __device__ __forceinline__ void codes_of(const float (&x)[8], const GroupDivider
     }
 }
 
-// PARO_ROWS: the codes of eight channels, the chunk-th eight of the group at `out`.
-template <int BITS>
-__device__ __forceinline__ void store_codes(uint8_t* out, int chunk, const float (&x)[8], const GroupDivider& quotient) {
+// PARO_ROWS: a lane's codes into its row of the group.
+template <int BITS, int D, bool HALVES>
+__device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x)[8], const GroupDivider& quotient) {
+    typedef LaneRow<float, D, HALVES> Lane;
+    const int first = Lane::first(L), second = first + Lane::SECOND;
     if constexpr (BITS == 16) {
-        unsigned h[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = f32_to_bf16_bits(x[e]);
-        uint4 w = make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
-        *(uint4*)(out + (size_t)chunk * 16) = w;
+        const unsigned v[4] = {f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16, f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16,
+                               f32_to_bf16_bits(x[4]) | f32_to_bf16_bits(x[5]) << 16, f32_to_bf16_bits(x[6]) | f32_to_bf16_bits(x[7]) << 16};
+        if constexpr (HALVES) {
+            *(uint2v*)(row + 2 * first) = (uint2v){v[0], v[1]};
+            *(uint2v*)(row + 2 * second) = (uint2v){v[2], v[3]};
+        } else {
+            *(uint4v*)(row + 2 * first) = (uint4v){v[0], v[1], v[2], v[3]};
+        }
     } else {
         int q[8];
         codes_of<BITS>(x, quotient, q);
         if constexpr (BITS == 8) {
-            uint2 w;
-            w.x = (q[0] & 0xff) | ((q[1] & 0xff) << 8) | ((q[2] & 0xff) << 16) | ((unsigned)q[3] << 24);
-            w.y = (q[4] & 0xff) | ((q[5] & 0xff) << 8) | ((q[6] & 0xff) << 16) | ((unsigned)q[7] << 24);
-            *(uint2*)(out + (size_t)chunk * 8) = w;
-        } else {
-            unsigned w = 0;
+            unsigned v[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w |= (unsigned)(q[e] & 0xf) << (4 * e);
-            *(unsigned*)(out + (size_t)chunk * 4) = w;
+            for (int i = 0; i < 2; ++i)
+                v[i] = (q[4 * i] & 0xff) | ((q[4 * i + 1] & 0xff) << 8) | ((q[4 * i + 2] & 0xff) << 16) | ((unsigned)q[4 * i + 3] << 24);
+            if constexpr (HALVES) {
+                *(unsigned*)(row + first) = v[0];
+                *(unsigned*)(row + second) = v[1];
+            } else {
+                *(uint2v*)(row + first) = (uint2v){v[0], v[1]};
+            }
+        } else {
+            unsigned v = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v |= (unsigned)(q[e] & 0xf) << (4 * e);
+            if constexpr (HALVES) {
+                *(uint16_t*)(row + first / 2) = (uint16_t)v;
+                *(uint16_t*)(row + second / 2) = (uint16_t)(v >> 16);
+            } else {
+                *(unsigned*)(row + first / 2) = v;
+            }
         }
     }
 }
 
-// PARO_VT: channels c0 .. c0 + 7 of token `row` of the block, into the staged tile.
-template <int BITS, int BLK>
-__device__ __forceinline__ void stage_codes(uint8_t* stage, int row, int c0, const float (&x)[8], const GroupDivider& quotient) {
+// PARO_VT: a lane's channels of token `token` of the block, into the staged tile.
+template <int BITS, int BLK, int D, bool HALVES>
+__device__ __forceinline__ void stage_codes(uint8_t* stage, int token, int L, const float (&x)[8], const GroupDivider& quotient) {
+    typedef LaneRow<float, D, HALVES> Lane;
+    const int slot = vt_slot(token);
+    int q[8];
     if constexpr (BITS == 16) {
-        unsigned h[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = f32_to_bf16_bits(x[e]);
-        uint16_t* st = (uint16_t*)stage;
-        const int slot = vt_slot(row);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) st[(c0 + e) * BLK + slot] = (uint16_t)h[e];
+        for (int e = 0; e < 8; ++e) q[e] = f32_to_bf16_bits(x[e]);
     } else {
-        int q[8];
         codes_of<BITS>(x, quotient, q);
-        const int slot = vt_slot(row);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) stage[(c0 + e) * stage_row<BITS, BLK>() + slot] = (uint8_t)q[e];
+    for (int e = 0; e < 8; ++e) {
+        const int at = (Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)) * stage_row<BITS, BLK>() + slot;
+        if constexpr (BITS == 16) ((uint16_t*)stage)[at] = (uint16_t)q[e];
+        else stage[at] = (uint8_t)q[e];
     }
 }
 
@@ -477,88 +505,105 @@ struct QuantArgs {
     Rows<const T> in[3];
     uint8_t* codes[3];
     float* scales[3];
-    int n_tokens, kblocks, nh;
+    int n_tokens, kblocks, nh, kind;
     double inv[6][2];  // per axis order: 1 / extent of the middle and of the fastest axis
     ReorderTable table;
 };
 
-// One workgroup owns one group of one tensor (grid: blocks, batches x heads, Q K V), one row per D / 16 lanes.
-template <typename T, int BLK, int D, int BITS, int LAYOUT>
+// Position in default order, and the grid coordinates, of the token at n_new of the head's sequence.
+struct Source {
+    int n, f, h, w;
+};
+template <typename T>
+__device__ __forceinline__ Source source_of(const QuantArgs<T>& a, const Turning& t, int order, int n_new) {
+    if (n_new >= t.n_img) return {n_new, 0, 0, 0};
+    const int* fwd = a.table.fwd[order];
+    const int q = quotient_of(n_new, a.inv[order][1]), c2 = n_new - q * fwd[1], c0 = quotient_of(q, a.inv[order][0]), c1 = q - c0 * fwd[0];
+    const AxisOrder axes = axis_order(order);
+    return {c0 * fwd[2] + c1 * fwd[3] + c2 * fwd[4], axes.a[0] == 0 ? c0 : axes.a[1] == 0 ? c1 : c2, axes.a[0] == 1 ? c0 : axes.a[1] == 1 ? c1 : c2,
+            axes.a[0] == 2 ? c0 : axes.a[1] == 2 ? c1 : c2};
+}
+
+// One workgroup owns one group of one tensor (grid: blocks, batches x heads, Q K V); the tile stays in registers between the pass for
+// the largest value and the codes.
+template <typename T, int BLK, int D, int BITS, int LAYOUT, bool HALVES>
 __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turning& t, const Norms& norm, int z) {
-    constexpr int LANES = D / 16, THREADS = BLK * LANES, WAVES = THREADS / 64, OUT_BYTES = BLK * D * BITS / 8;
+    constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8;
     constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
     __shared__ __attribute__((aligned(16))) uint8_t stage[LAYOUT == PARO_VT ? stage_bytes<BITS, BLK, D>() : 16];
-    __shared__ float wave_amax[WAVES];
+    __shared__ float wave_amax[kThreads / 64];
     const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, blk = blockIdx.x, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
     const size_t group = (size_t)bh * a.kblocks + blk;
-    const int n_new = blk * BLK + row;
-    float y[16];
+    const int order = a.table.perm[h];
+    LaneRow<T, D, HALVES> x[IT];
+    Source from[IT];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) y[e] = 0.0f;
-    if (n_new < a.n_tokens) {
-        int n = n_new, f = 0, hg = 0, w = 0;
-        if (n_new < t.n_img) {
-            const int order = a.table.perm[h];
-            const int* fwd = a.table.fwd[order];
-            const int q = quotient_of(n_new, a.inv[order][1]), c2 = n_new - q * fwd[1], c0 = quotient_of(q, a.inv[order][0]), c1 = q - c0 * fwd[0];
-            n = c0 * fwd[2] + c1 * fwd[3] + c2 * fwd[4];
-            const AxisOrder axes = axis_order(order);
-            f = axes.a[0] == 0 ? c0 : axes.a[1] == 0 ? c1 : c2;
-            hg = axes.a[0] == 1 ? c0 : axes.a[1] == 1 ? c1 : c2;
-            w = axes.a[0] == 2 ? c0 : axes.a[1] == 2 ? c1 : c2;
+    for (int it = 0; it < IT; ++it) {
+        const int n_new = blk * BLK + it * ROWS + row;
+        if (n_new < a.n_tokens) {
+            from[it] = source_of(a, t, order, n_new);
+            x[it].load(a.in[z].row(b, h, from[it].n), L);
         }
-        LaneRow<T> x;
-        x.template load<D>(a.in[z].row(b, h, n), L);
-        if (LAYOUT == PARO_VT) {
+    }
+    float y[IT][8], amax = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = x[e];
-        } else {
-            LaneTurn angles;
-            if (n_new < t.n_img && t.total) angles = load_turn<D>(t, L, f, hg, w);
-            else angles = turn_of_token<D>(t, L, t.n_img);
-            if (norm.kind == PARO_NORM_NONE) {
-                normed_and_turned<D, false>(x, norm, y, y, angles, t.halves, y);
+    for (int it = 0; it < IT; ++it) {
+        const int n_new = blk * BLK + it * ROWS + row;
+        if (n_new < a.n_tokens) {
+            if constexpr (LAYOUT == PARO_VT) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[it][e] = x[it][e];
             } else {
-                float weight[16], bias[16];
                 const int text = n_new >= t.n_img;
-                load_vector<D>(norm.w[z][text], L, 1.0f, weight);
-                load_vector<D>(norm.b[z][text], L, 0.0f, bias);
-                normed_and_turned<D, true>(x, norm, weight, bias, angles, t.halves, y);
+                LaneTurn angles;
+                if (!text && t.total) load_turn(t, L, from[it].f, from[it].h, from[it].w, angles);
+                else angles.none();
+                float w[8], bias[8];
+                if (a.kind == PARO_NORM_NONE) {
+                    normed_and_turned<PARO_NORM_NONE>(x[it], norm.eps, w, bias, angles, y[it]);
+                } else {
+                    load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
+                    if (a.kind == PARO_NORM_RMS) {
+                        normed_and_turned<PARO_NORM_RMS>(x[it], norm.eps, w, bias, angles, y[it]);
+                    } else {
+                        load_vector<D, HALVES>(norm.b[z][text], L, 0.0f, bias);
+                        normed_and_turned<PARO_NORM_LAYER>(x[it], norm.eps, w, bias, angles, y[it]);
+                    }
+                }
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[it][e] = 0.0f;
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e]));
     }
     float scale = 1.0f;
     if constexpr (BITS != 16) {
-        float amax = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(y[e]));
         amax = wave_max(amax);
         if ((tid & 63) == 0) wave_amax[tid >> 6] = amax;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) amax = fmaxf(amax, wave_amax[i]);
+        amax = fmaxf(fmaxf(wave_amax[0], wave_amax[1]), fmaxf(wave_amax[2], wave_amax[3]));
         if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
     }
     if (tid == 0) a.scales[z][group] = scale;
     const GroupDivider quotient(scale);
     uint8_t* out = a.codes[z] + group * OUT_BYTES;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int c0 = half * (D / 2) + 8 * L;
-        const float(&v)[8] = *(const float(*)[8])(y + 8 * half);
-        if constexpr (LAYOUT == PARO_ROWS) store_codes<BITS>(out, row * (D / 8) + c0 / 8, v, quotient);
-        else stage_codes<BITS, BLK>(stage, row, c0, v, quotient);
+    for (int it = 0; it < IT; ++it) {
+        if constexpr (LAYOUT == PARO_ROWS) store_codes<BITS, D, HALVES>(out + (it * ROWS + row) * (D * BITS / 8), L, y[it], quotient);
+        else stage_codes<BITS, BLK, D, HALVES>(stage, it * ROWS + row, L, y[it], quotient);
     }
     if constexpr (LAYOUT == PARO_VT) {
         __syncthreads();
-        store_staged<BITS, BLK, D, THREADS>(out, stage, tid);
+        store_staged<BITS, BLK, D, kThreads>(out, stage, tid);
     }
 }
 
-template <typename T, int BLK, int D, int QKBITS, int PVBITS>
-__global__ __launch_bounds__(BLK * D / 16) void norm_rope_quantize_kernel(QuantArgs<T> a, Turning t, Norms norm) {
-    if (blockIdx.z < 2) quantize_rows<T, BLK, D, QKBITS, PARO_ROWS>(a, t, norm, blockIdx.z);
-    else quantize_rows<T, BLK, D, PVBITS, PARO_VT>(a, t, norm, 2);
+template <typename T, int BLK, int D, int QKBITS, int PVBITS, bool HALVES>
+__global__ __launch_bounds__(kThreads) void norm_rope_quantize_kernel(QuantArgs<T> a, Turning t, Norms norm) {
+    if (blockIdx.z < 2) quantize_rows<T, BLK, D, QKBITS, PARO_ROWS, HALVES>(a, t, norm, blockIdx.z);
+    else quantize_rows<T, BLK, D, PVBITS, PARO_VT, false>(a, t, norm, 2);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -597,11 +642,13 @@ static int make_turning(const paro_shape* s, const paro_rope_axes* axes, const f
     t->total = (axes->dims[0] + axes->dims[1] + axes->dims[2]) / 2;
     if (t->total && !table) return fail(PARO_EINVAL, "table is NULL");
     if (misaligned(table)) return fail(PARO_EINVAL, "table must be 16-byte aligned");
-    t->table = (const float2*)table;
+    t->table = table;
+    t->fours = true;
     const int extent[3] = {s->F, s->Hg, s->Wg};
     int64_t at = 0;
     for (int a = 0; a < 3; ++a) {
         t->pairs[a] = axes->dims[a] / 2;
+        t->fours = t->fours && t->pairs[a] % 4 == 0;
         t->base[a] = (int)at;
         at += (int64_t)extent[a] * t->pairs[a];
     }
@@ -611,7 +658,6 @@ static int make_turning(const paro_shape* s, const paro_rope_axes* axes, const f
     t->inv_hg = 1.0 / s->Hg;
     t->inv_wg = 1.0 / s->Wg;
     t->sign = back ? -1.0f : 1.0f;
-    t->halves = axes->pairs == PARO_PAIRS_HALVES;
     return PARO_OK;
 }
 
@@ -620,7 +666,6 @@ static int make_norms(const paro_qk_norm* norm, Norms* out) {
     if (norm->kind != PARO_NORM_NONE && norm->kind != PARO_NORM_RMS && norm->kind != PARO_NORM_LAYER)
         return fail(PARO_EINVAL, "norm kind=%d is not a paro_norm_kind", (int)norm->kind);
     if (norm->kind != PARO_NORM_NONE && !(norm->eps >= 0.0 && norm->eps < INFINITY)) return fail(PARO_EINVAL, "eps=%g must be finite and >= 0", norm->eps);
-    out->kind = norm->kind;
     out->eps = norm->eps;
     for (int i = 0; i < 2; ++i) {
         if (norm->kind == PARO_NORM_NONE && (norm->weight[i] || norm->text_weight[i])) return fail(PARO_EINVAL, "weights need a norm");
@@ -645,35 +690,51 @@ static int heads_per_group(const paro_shape* s, int64_t tiles, int tensors) {
     return heads;
 }
 
-static int tile_tokens(const paro_shape* s) { return kThreads / (s->d / 16); }
+static int tile_tokens(const paro_shape* s) { return kThreads / (s->d / 8); }
 
 static int check_dtype(paro_dtype dtype) {
     if (dtype != PARO_F32 && dtype != PARO_BF16) return fail(PARO_EINVAL, "dtype=%d is not a paro_dtype", (int)dtype);
     return PARO_OK;
 }
 
-template <typename T, int D>
-static void launch_rows(bool norm, dim3 grid, hipStream_t st, const RowsArgs<T>& a, const Turning& t, const Norms& n) {
-    if (norm) hipLaunchKernelGGL((rotate_rows_kernel<T, D, true>), grid, dim3(kThreads), 0, st, a, t, n);
-    else hipLaunchKernelGGL((rotate_rows_kernel<T, D, false>), grid, dim3(kThreads), 0, st, a, t, n);
+// f(T, D, KIND, HALVES) of a call, as compile-time constants.
+template <typename F>
+static void with_kernel(const paro_shape* s, paro_dtype dtype, int kind, int pairs, F&& f) {
+    auto of_pairs = [&](auto t, auto d, auto k) {
+        if (pairs == PARO_PAIRS_HALVES) f(t, d, k, std::true_type());
+        else f(t, d, k, std::false_type());
+    };
+    auto of_kind = [&](auto t, auto d) {
+        if (kind == PARO_NORM_NONE) of_pairs(t, d, std::integral_constant<int, PARO_NORM_NONE>());
+        else if (kind == PARO_NORM_RMS) of_pairs(t, d, std::integral_constant<int, PARO_NORM_RMS>());
+        else of_pairs(t, d, std::integral_constant<int, PARO_NORM_LAYER>());
+    };
+    auto of_d = [&](auto t) {
+        if (s->d == 64) of_kind(t, std::integral_constant<int, 64>());
+        else of_kind(t, std::integral_constant<int, 128>());
+    };
+    if (dtype == PARO_F32) of_d(float());
+    else of_d(uint16_t());
 }
 
-template <typename T>
-static void launch_forward(const paro_shape* s, int64_t n, int tensors, const paro_strided* const (&in)[2], const paro_strided* const (&out)[2],
-                           const Turning& t, const Norms& norm, hipStream_t st) {
-    RowsArgs<T> a;
-    memset(&a, 0, sizeof(a));
-    for (int i = 0; i < tensors; ++i) {
-        a.in[i] = rows_of<const T>(in[i]);
-        a.out[i] = rows_of<T>(out[i]);
-    }
+static void launch_forward(const paro_shape* s, int64_t n, paro_dtype dtype, int kind, int pairs, int tensors, const paro_strided* const (&in)[2],
+                           const paro_strided* const (&out)[2], const Turning& t, const Norms& norm, hipStream_t st) {
     const int64_t tiles = (n + tile_tokens(s) - 1) / tile_tokens(s);
-    a.n_tokens = (int)n;
-    a.nh = s->nh;
-    a.heads = heads_per_group(s, tiles, tensors);
-    const dim3 grid((unsigned)tiles, (unsigned)(s->B * ((s->nh + a.heads - 1) / a.heads)), (unsigned)tensors);
-    if (s->d == 64) launch_rows<T, 64>(norm.kind != PARO_NORM_NONE, grid, st, a, t, norm);
-    else launch_rows<T, 128>(norm.kind != PARO_NORM_NONE, grid, st, a, t, norm);
+    const int heads = heads_per_group(s, tiles, tensors);
+    const dim3 grid((unsigned)tiles, (unsigned)(s->B * ((s->nh + heads - 1) / heads)), (unsigned)tensors);
+    with_kernel(s, dtype, kind, pairs, [&](auto t0, auto d, auto k, auto halves) {
+        typedef decltype(t0) T;
+        RowsArgs<T> a;
+        memset(&a, 0, sizeof(a));
+        for (int i = 0; i < tensors; ++i) {
+            a.in[i] = rows_of<const T>(in[i]);
+            a.out[i] = rows_of<T>(out[i]);
+        }
+        a.n_tokens = (int)n;
+        a.nh = s->nh;
+        a.heads = heads;
+        hipLaunchKernelGGL((rotate_rows_kernel<T, d(), k(), halves()>), grid, dim3(kThreads), 0, st, a, t, norm);
+    });
 }
 
 // What the gradient's partial sums take: tiles of image and of text tokens, and the groups of heads.
@@ -692,30 +753,32 @@ static GradSplit grad_split(const paro_shape* s) {
     return g;
 }
 
-template <typename T>
-static void launch_grad(const paro_shape* s, int64_t n, const GradSplit& split, const paro_strided* const (&x)[2], const paro_strided* const (&dy)[2],
-                        const paro_strided* const (&dx)[2], float* partial, const Turning& t, const Norms& norm, hipStream_t st) {
-    GradArgs<T> a;
-    for (int i = 0; i < 2; ++i) {
-        a.x[i] = rows_of<const T>(x[i]);
-        a.dy[i] = rows_of<const T>(dy[i]);
-        a.dx[i] = rows_of<T>(dx[i]);
-    }
-    a.partial = partial;
-    a.n_tokens = (int)n;
-    a.nh = s->nh;
-    a.heads = split.heads;
-    a.img_tiles = (int)split.img_tiles;
+static void launch_grad(const paro_shape* s, int64_t n, paro_dtype dtype, int kind, int pairs, const GradSplit& split, const paro_strided* const (&x)[2],
+                        const paro_strided* const (&dy)[2], const paro_strided* const (&dx)[2], float* partial, const Turning& t, const Norms& norm,
+                        hipStream_t st) {
     const dim3 grid((unsigned)split.tiles, (unsigned)(s->B * split.groups), 2);
-    if (s->d == 64) hipLaunchKernelGGL((norm_rope_grad_kernel<T, 64>), grid, dim3(kThreads), 0, st, a, t, norm);
-    else hipLaunchKernelGGL((norm_rope_grad_kernel<T, 128>), grid, dim3(kThreads), 0, st, a, t, norm);
+    with_kernel(s, dtype, kind, pairs, [&](auto t0, auto d, auto k, auto halves) {
+        typedef decltype(t0) T;
+        GradArgs<T> a;
+        for (int i = 0; i < 2; ++i) {
+            a.x[i] = rows_of<const T>(x[i]);
+            a.dy[i] = rows_of<const T>(dy[i]);
+            a.dx[i] = rows_of<T>(dx[i]);
+        }
+        a.partial = partial;
+        a.n_tokens = (int)n;
+        a.nh = s->nh;
+        a.heads = split.heads;
+        a.img_tiles = (int)split.img_tiles;
+        hipLaunchKernelGGL((norm_rope_grad_kernel<T, d(), k(), halves()>), grid, dim3(kThreads), 0, st, a, t, norm);
+    });
 }
 
-template <typename T, int BLK, int D>
+template <typename T, int BLK, int D, bool HALVES>
 static bool launch_quant_bits(int bits_qk, int bits_pv, dim3 grid, hipStream_t st, const QuantArgs<T>& a, const Turning& t, const Norms& norm) {
 #define PARO_QKV_CASE(QK, PV)                                                                                                             \
     if (bits_qk == QK && bits_pv == PV) {                                                                                                 \
-        hipLaunchKernelGGL((norm_rope_quantize_kernel<T, BLK, D, QK, PV>), grid, dim3(BLK * D / 16), 0, st, a, t, norm);                  \
+        hipLaunchKernelGGL((norm_rope_quantize_kernel<T, BLK, D, QK, PV, HALVES>), grid, dim3(kThreads), 0, st, a, t, norm);            \
         return true;                                                                                                                      \
     }
     PARO_QKV_CASE(8, 8)
@@ -727,16 +790,16 @@ static bool launch_quant_bits(int bits_qk, int bits_pv, dim3 grid, hipStream_t s
     return false;
 }
 
-template <typename T>
+template <typename T, bool HALVES>
 static bool launch_quant(const paro_shape* s, int bits_qk, int bits_pv, dim3 grid, hipStream_t st, const QuantArgs<T>& a, const Turning& t, const Norms& norm) {
-    if (s->block == 64 && s->d == 64) return launch_quant_bits<T, 64, 64>(bits_qk, bits_pv, grid, st, a, t, norm);
-    if (s->block == 64) return launch_quant_bits<T, 64, 128>(bits_qk, bits_pv, grid, st, a, t, norm);
-    if (s->d == 64) return launch_quant_bits<T, 32, 64>(bits_qk, bits_pv, grid, st, a, t, norm);
-    return launch_quant_bits<T, 32, 128>(bits_qk, bits_pv, grid, st, a, t, norm);
+    if (s->block == 64 && s->d == 64) return launch_quant_bits<T, 64, 64, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
+    if (s->block == 64) return launch_quant_bits<T, 64, 128, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
+    if (s->d == 64) return launch_quant_bits<T, 32, 64, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
+    return launch_quant_bits<T, 32, 128, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
 }
 
 template <typename T>
-static int quantize_entry(const paro_shape* s, int64_t n, int64_t kb, int bits_qk, int bits_pv, const uint8_t* h_perm_ids, const paro_strided* const (&in)[3],
+static int quantize_entry(const paro_shape* s, int64_t n, int64_t kb, int kind, int pairs, int bits_qk, int bits_pv, const uint8_t* h_perm_ids, const paro_strided* const (&in)[3],
                           void* const (&codes)[3], float* const (&scales)[3], const Turning& t, const Norms& norm, hipStream_t st) {
     QuantArgs<T> a;
     if (int e = make_reorder_table(s, h_perm_ids, &a.table)) return e;
@@ -750,7 +813,9 @@ static int quantize_entry(const paro_shape* s, int64_t n, int64_t kb, int bits_q
     a.n_tokens = (int)n;
     a.kblocks = (int)kb;
     a.nh = s->nh;
-    if (!launch_quant<T>(s, bits_qk, bits_pv, dim3((unsigned)kb, (unsigned)(s->B * s->nh), 3), st, a, t, norm))
+    a.kind = kind;
+    const auto run = pairs == PARO_PAIRS_HALVES ? launch_quant<T, true> : launch_quant<T, false>;
+    if (!run(s, bits_qk, bits_pv, dim3((unsigned)kb, (unsigned)(s->B * s->nh), 3), st, a, t, norm))
         return fail(PARO_EINVAL, "bits (qk=%d, pv=%d): expected (8,8), (8,4), (4,4), (4,8) or (16,16)", bits_qk, bits_pv);
     return check_launch("paro_qk_norm_rope_quantize_qkv");
 }
@@ -771,8 +836,7 @@ extern "C" int paro_rope(const paro_shape* s, paro_dtype dtype, const paro_rope_
     if (x->data == y->data && !same_rows(s, n, x, y)) return fail(PARO_EINVAL, "y lies in the memory of x in another order");
     Norms none;
     memset(&none, 0, sizeof(none));
-    if (dtype == PARO_F32) launch_forward<float>(s, n, 1, {x, nullptr}, {y, nullptr}, t, none, (hipStream_t)stream);
-    else launch_forward<uint16_t>(s, n, 1, {x, nullptr}, {y, nullptr}, t, none, (hipStream_t)stream);
+    launch_forward(s, n, dtype, PARO_NORM_NONE, axes->pairs, 1, {x, nullptr}, {y, nullptr}, t, none, (hipStream_t)stream);
     return check_launch("paro_rope");
 }
 
@@ -792,8 +856,7 @@ extern "C" int paro_qk_norm_rope(const paro_shape* s, paro_dtype dtype, const pa
     if (q_out->data == k_out->data || q_out->data == k->data || k_out->data == q->data || (q_out->data == q->data && !same_rows(s, n, q, q_out)) ||
         (k_out->data == k->data && !same_rows(s, n, k, k_out)))
         return fail(PARO_EINVAL, "an output may be its own input in the same order, and none of the other tensors");
-    if (dtype == PARO_F32) launch_forward<float>(s, n, 2, {q, k}, {q_out, k_out}, t, norms, (hipStream_t)stream);
-    else launch_forward<uint16_t>(s, n, 2, {q, k}, {q_out, k_out}, t, norms, (hipStream_t)stream);
+    launch_forward(s, n, dtype, norm->kind, axes->pairs, 2, {q, k}, {q_out, k_out}, t, norms, (hipStream_t)stream);
     return check_launch("paro_qk_norm_rope");
 }
 
@@ -849,8 +912,7 @@ extern "C" int paro_qk_norm_rope_backward(const paro_shape* s, paro_dtype dtype,
     if (count && (!scratch || misaligned(scratch))) return fail(PARO_EINVAL, "scratch must be a 16-byte aligned buffer");
     const auto st = (hipStream_t)stream;
     float* const partial = count ? (float*)scratch : nullptr;
-    if (dtype == PARO_F32) launch_grad<float>(s, n, split, x, dy, dx, partial, t, norms, st);
-    else launch_grad<uint16_t>(s, n, split, x, dy, dx, partial, t, norms, st);
+    launch_grad(s, n, dtype, norm->kind, axes->pairs, split, x, dy, dx, partial, t, norms, st);
     if (int e = check_launch("paro_qk_norm_rope_backward")) return e;
     if (count) {
         if (s->d == 64) hipLaunchKernelGGL((norm_grad_kernel<64>), dim3(count), dim3(1024), 0, st, partial, slots, jobs);
@@ -885,6 +947,6 @@ extern "C" int paro_qk_norm_rope_quantize_qkv(const paro_shape* s, paro_dtype dt
             if (codes[i] == in[j]->data || (i != j && codes[i] == codes[j]) || (i != j && scales[i] == scales[j]))
                 return fail(PARO_EINVAL, "inputs and outputs must not alias");
     const auto st = (hipStream_t)stream;
-    if (dtype == PARO_F32) return quantize_entry<float>(s, n, kb, bits_qk, bits_pv, h_perm_ids, in, codes, scales, t, norms, st);
-    return quantize_entry<uint16_t>(s, n, kb, bits_qk, bits_pv, h_perm_ids, in, codes, scales, t, norms, st);
+    if (dtype == PARO_F32) return quantize_entry<float>(s, n, kb, norm->kind, axes->pairs, bits_qk, bits_pv, h_perm_ids, in, codes, scales, t, norms, st);
+    return quantize_entry<uint16_t>(s, n, kb, norm->kind, axes->pairs, bits_qk, bits_pv, h_perm_ids, in, codes, scales, t, norms, st);
 }

@@ -163,7 +163,7 @@ def _abs_turn(x, p):
 
 def _bounds(p, which, x, dy):
     """dx = r (g w - m1 - h m2) in binary32: g from one product and one fma (2 roundings of its terms A), g w one more, h one, the two
-    means sums of d terms, at most 16 in a lane, 3 steps across lanes and the factor 1/d: 20 roundings each, of terms v (3 roundings) or v h
+    means sums of d terms, 8 in a lane, at most 4 steps across lanes and the factor 1/d: 13 roundings each, of terms v (3 roundings) or v h
     (5); then h m2, the differences, the factor r: 4.  28 roundings of the terms' absolute values cover each part.  A weight's
     gradient adds g h (4 roundings) over the heads of a workgroup (at most nh) in binary32, the rest in binary64 with two roundings to
     binary32 on the way."""
