@@ -141,6 +141,16 @@ __device__ __forceinline__ V row_sum(V v) {
     return v;
 }
 
+// Sum over the rows of a wavefront, lane by lane of a row: lanes 8 (d = 64), 16 and 32 apart.
+template <int D>
+__device__ __forceinline__ float rows_sum(float v) {
+    if constexpr (D == 64) v += moved<0x128>(v);  // row_ror:8
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // 1 / sqrt(v): the instruction's estimate and two Newton steps, y <- y + y (1/2 - v/2 y^2), which square its relative error.  The
 // estimate stands where v is 0 or infinite.
 __device__ __forceinline__ double rsqrt_of(double v) {
@@ -352,21 +362,26 @@ __global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(GradArgs<T> a,
         }
     }
     if (KIND == PARO_NORM_NONE || !a.partial) return;
-    // the workgroup's sums: [channel][token row], one row more against bank conflicts
-    __shared__ float meet[D][TOKENS + 1];
+    // the workgroup's sums: over the rows of a wavefront, then over the wavefronts
+    constexpr int KINDS = KIND == PARO_NORM_LAYER ? 2 : 1, WAVES = kThreads / 64;
+    __shared__ float meet[WAVES][KINDS][D];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int kind = 0; kind < KINDS; ++kind)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float s = rows_sum<D>(kind ? db[e] : dw[e]);
+            if (lane < LANES) meet[wave][kind][Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)] = s;
+        }
+    __syncthreads();
     const size_t slot = (size_t)blockIdx.x * gridDim.y + blockIdx.y, slots = (size_t)gridDim.x * gridDim.y;
     float* out = a.partial + (z * slots + slot) * (2 * D);
+    if (threadIdx.x < KINDS * D) {
+        const int kind = threadIdx.x / D, c = threadIdx.x % D;
+        double s = 0.0;
 #pragma unroll
-    for (int kind = 0; kind < (KIND == PARO_NORM_LAYER ? 2 : 1); ++kind) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) meet[Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)][row] = kind ? db[e] : dw[e];
-        __syncthreads();
-        if (threadIdx.x < D) {
-            double s = 0.0;
-            for (int i = 0; i < TOKENS; ++i) s += (double)meet[threadIdx.x][i];
-            out[kind * D + threadIdx.x] = (float)s;
-        }
+        for (int i = 0; i < WAVES; ++i) s += (double)meet[i][kind][c];
+        out[threadIdx.x] = (float)s;
     }
 }
 
@@ -380,19 +395,28 @@ struct GradJobs {
     GradJob job[8];
 };
 
+// grid: (jobs, D / 16).  A workgroup adds up 16 channels of a job's slots, 64 slots at a time, in binary64 and in a fixed order; four loads a
+// thread are in flight.
 template <int D>
 __global__ __launch_bounds__(1024) void norm_grad_kernel(const float* __restrict__ partial, int64_t slots, GradJobs jobs) {
-    constexpr int PARTS = 1024 / D;
-    __shared__ double meet[PARTS][D];
+    constexpr int PARTS = 64;
+    __shared__ double meet[PARTS][16];
     const GradJob j = jobs.job[blockIdx.x];
-    const int c = threadIdx.x % D, part = threadIdx.x / D;
+    const int c = threadIdx.x % 16, part = threadIdx.x / 16;
+    const float* mine = partial + (j.tensor * slots * 2 + j.kind) * D + blockIdx.y * 16 + c;
     double s = 0.0;
-    for (int64_t i = j.first + part; i < j.last; i += PARTS) s += (double)partial[((j.tensor * slots + i) * 2 + j.kind) * D + c];
+#pragma unroll 4
+    for (int64_t i = j.first + part; i < j.last; i += PARTS) s += (double)mine[i * (2 * D)];
     meet[part][c] = s;
     __syncthreads();
+    if (part < 8) {
+        for (int i = 8; i < PARTS; i += 8) s += meet[part + i][c];
+        meet[part][c] = s;  // no other thread reads this entry before the barrier
+    }
+    __syncthreads();
     if (part == 0) {
-        for (int i = 1; i < PARTS; ++i) s += meet[i][c];
-        j.out[c] = (float)s;
+        for (int i = 1; i < 8; ++i) s += meet[i][c];
+        j.out[blockIdx.y * 16 + c] = (float)s;
     }
 }
 
@@ -683,11 +707,22 @@ static int make_norms(const paro_qk_norm* norm, Norms* out) {
 template <typename T>
 static Rows<T> rows_of(const paro_strided* r) { return {(T*)r->data, r->batch, r->head, r->token}; }
 
-// Heads that a workgroup goes through: all of them as soon as there are 2048 workgroups without splitting them, else as few as it takes.
-static int heads_per_group(const paro_shape* s, int64_t tiles, int tensors) {
+// Heads that a workgroup goes through: so few that there are `least` workgroups (below that a launch lasts as long as a workgroup), and
+// not more than three while there are fewer than `enough`.
+static int heads_per_group(const paro_shape* s, int64_t tiles, int tensors, int least, int enough) {
     int heads = s->nh;
-    while (heads > 1 && tiles * tensors * s->B * ((s->nh + heads - 1) / heads) < 2048) heads = (heads + 1) / 2;
+    const auto workgroups = [&] { return tiles * tensors * s->B * ((s->nh + heads - 1) / heads); };
+    while (heads > 1 && workgroups() < least) heads = (heads + 1) / 2;
+    while (heads > 3 && workgroups() < enough) heads = (heads + 1) / 2;
     return heads;
+}
+
+// Forward: four workgroups for each compute unit before anything else.  With fewer heads a workgroup's angles and weights cost more than
+// its rows (24 heads of 4608 tokens, d = 128, rotation: one head 15.1 us, three 11.9, six 11.5), with more a launch ends unevenly (48
+// heads of 17550 tokens, d = 64, rotation: three 44.8, six 46.2, twelve 49.8; Q and K with root-mean-square norms six 86.8, twelve 88.0, 24
+// 90.6; with layer norms, which hold more per lane, six 93.8, twelve 91.5, 24 94.6).
+static int forward_heads(const paro_shape* s, int64_t tiles, int tensors, int kind) {
+    return heads_per_group(s, tiles, tensors, 1024, kind == PARO_NORM_LAYER ? 4096 : 8192);
 }
 
 static int tile_tokens(const paro_shape* s) { return kThreads / (s->d / 8); }
@@ -720,7 +755,7 @@ static void with_kernel(const paro_shape* s, paro_dtype dtype, int kind, int pai
 static void launch_forward(const paro_shape* s, int64_t n, paro_dtype dtype, int kind, int pairs, int tensors, const paro_strided* const (&in)[2],
                            const paro_strided* const (&out)[2], const Turning& t, const Norms& norm, hipStream_t st) {
     const int64_t tiles = (n + tile_tokens(s) - 1) / tile_tokens(s);
-    const int heads = heads_per_group(s, tiles, tensors);
+    const int heads = forward_heads(s, tiles, tensors, kind);
     const dim3 grid((unsigned)tiles, (unsigned)(s->B * ((s->nh + heads - 1) / heads)), (unsigned)tensors);
     with_kernel(s, dtype, kind, pairs, [&](auto t0, auto d, auto k, auto halves) {
         typedef decltype(t0) T;
@@ -748,7 +783,9 @@ static GradSplit grad_split(const paro_shape* s) {
     const int64_t tile = tile_tokens(s), n_img = (int64_t)s->F * s->Hg * s->Wg;
     g.img_tiles = (n_img + tile - 1) / tile;
     g.tiles = g.img_tiles + (s->T_text + tile - 1) / tile;
-    g.heads = heads_per_group(s, g.tiles, 2);
+    // fewer workgroups than forward: each leaves partial sums (12 fp32 heads of 1955 tokens: at least 256 workgroups 12.9 us, 1024 16.1;
+    // 24 bf16 heads of 4608, d = 128: 1024 38.4, 2048 39.5; 48 of 17550, d = 64: the same within 2 %)
+    g.heads = heads_per_group(s, g.tiles, 2, 256, 1024);
     g.groups = (s->nh + g.heads - 1) / g.heads;
     return g;
 }
@@ -915,8 +952,8 @@ extern "C" int paro_qk_norm_rope_backward(const paro_shape* s, paro_dtype dtype,
     launch_grad(s, n, dtype, norm->kind, axes->pairs, split, x, dy, dx, partial, t, norms, st);
     if (int e = check_launch("paro_qk_norm_rope_backward")) return e;
     if (count) {
-        if (s->d == 64) hipLaunchKernelGGL((norm_grad_kernel<64>), dim3(count), dim3(1024), 0, st, partial, slots, jobs);
-        else hipLaunchKernelGGL((norm_grad_kernel<128>), dim3(count), dim3(1024), 0, st, partial, slots, jobs);
+        if (s->d == 64) hipLaunchKernelGGL((norm_grad_kernel<64>), dim3(count, 4), dim3(1024), 0, st, partial, slots, jobs);
+        else hipLaunchKernelGGL((norm_grad_kernel<128>), dim3(count, 8), dim3(1024), 0, st, partial, slots, jobs);
     }
     return check_launch("paro_qk_norm_rope_backward");
 }
