@@ -44,8 +44,9 @@ struct Norms {
 template <typename T>
 struct Rows {
     T* p;
-    int64_t batch, head, token;
-    __device__ T* row(int b, int h, int n) const { return p + b * batch + h * head + n * token; }
+    int64_t batch, head;
+    int token;
+    __device__ T* row(int b, int h, int n) const { return p + b * batch + h * head + (int64_t)n * token; }
 };
 
 // floor(n / divisor) for 0 <= n < 2^24 and a divisor of at most that, inv = fl64(1 / divisor): (n + 1/2) inv lies 1 / (2 divisor)
@@ -87,6 +88,10 @@ struct LaneRow {
                 }
             }
         }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
     }
     __device__ __forceinline__ float operator[](int e) const {
         if constexpr (sizeof(T) == 2) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
@@ -161,23 +166,21 @@ __device__ __forceinline__ double rsqrt_of(double v) {
     return v > 0.0 && v < __builtin_inf() ? y : y0;
 }
 
-// What a row is normalised by: value e becomes (x[e] - mean) r.
-template <int KIND, typename T, int D, bool HALVES>
-__device__ __forceinline__ void row_norm(const LaneRow<T, D, HALVES>& x, double eps, double& mean, double& r) {
-    mean = 0.0;
-    if constexpr (KIND == PARO_NORM_LAYER) {
+// What a row is divided by; under PARO_NORM_LAYER its values lose their mean first.
+template <int D>
+__device__ __forceinline__ double row_norm(double (&u)[8], int kind, double eps) {
+    if (kind == PARO_NORM_LAYER) {
         double s = 0.0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += (double)x[e];
-        mean = row_sum<D>(s) * (1.0 / D);
+        for (int e = 0; e < 8; ++e) s += u[e];
+        s = row_sum<D>(s) * (1.0 / D);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] -= s;
     }
     double s = 0.0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const double v = (double)x[e] - mean;
-        s = fma(v, v, s);
-    }
-    r = rsqrt_of(fma(row_sum<D>(s), 1.0 / D, eps));
+    for (int e = 0; e < 8; ++e) s = fma(u[e], u[e], s);
+    return rsqrt_of(fma(row_sum<D>(s), 1.0 / D, eps));
 }
 
 // ---- turning -------------------------------------------------------------------------------------------------------
@@ -227,33 +230,40 @@ __device__ __forceinline__ void turn_of_token(const Turning& t, int L, int n, La
     }
 }
 
-// A value that does not turn stays as it is, whatever its partner holds; a wavefront whose pairs all turn needs no selection.
+template <typename V>
+__device__ __forceinline__ void turn_pair(V& x, V& y, V c, V s) {
+    const V a = fma(x, c, -(y * s));
+    y = fma(x, s, y * c);
+    x = a;
+}
+// A value that does not turn stays as it is, whatever its partner holds.
 template <bool HALVES, typename V>
 __device__ __forceinline__ void turn_lane(V (&u)[8], const LaneTurn& t) {
-    const bool all = __all(t.turned == 15);
+    if (t.turned == 15) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        V &x = HALVES ? u[e] : u[2 * e], &y = HALVES ? u[4 + e] : u[2 * e + 1];
-        const V c = t.c[e], s = t.s[e], a = fma(x, c, -(y * s)), b = fma(x, s, y * c);
-        if (all || (t.turned >> e & 1)) x = a, y = b;
+        for (int e = 0; e < 4; ++e) turn_pair<V>(HALVES ? u[e] : u[2 * e], HALVES ? u[4 + e] : u[2 * e + 1], t.c[e], t.s[e]);
+    } else if (t.turned) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (t.turned >> e & 1) turn_pair<V>(HALVES ? u[e] : u[2 * e], HALVES ? u[4 + e] : u[2 * e + 1], t.c[e], t.s[e]);
     }
 }
 
-// The row behind norm and rotation, rounded to binary32.
-template <int KIND, typename T, int D, bool HALVES>
-__device__ __forceinline__ void normed_and_turned(const LaneRow<T, D, HALVES>& x, double eps, const float (&w)[8], const float (&b)[8], const LaneTurn& t,
-                                                  float (&y)[8]) {
+// The row behind norm and rotation, rounded to binary32.  w and b: 1 and -0 where there is nothing (exact, signs of zeros included).
+template <typename T, int D, bool HALVES>
+__device__ __forceinline__ void normed_and_turned(const LaneRow<T, D, HALVES>& x, int kind, double eps, const float (&w)[8], const float (&b)[8],
+                                                  const LaneTurn& t, float (&y)[8]) {
     double u[8];
-    if constexpr (KIND == PARO_NORM_NONE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = (double)x[e];
-    } else {
-        double mean, r;
-        row_norm<KIND>(x, eps, mean, r);
+    for (int e = 0; e < 8; ++e) u[e] = (double)x[e];
+    if (kind != PARO_NORM_NONE) {
+        const double r = row_norm<D>(u, kind, eps);
+        if (kind == PARO_NORM_LAYER) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double v = ((double)x[e] - mean) * r;
-            u[e] = KIND == PARO_NORM_LAYER ? fma(v, (double)w[e], (double)b[e]) : v * (double)w[e];
+            for (int e = 0; e < 8; ++e) u[e] = fma(u[e] * r, (double)w[e], (double)b[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = u[e] * r * (double)w[e];
         }
     }
     turn_lane<HALVES>(u, t);
@@ -289,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(RowsArgs<T> a, Tu
         const LaneRow<T, D, HALVES> x = next;
         if (h + 1 < h1) next.load(a.in[z].row(b, h + 1, n), L);
         float y[8];
-        normed_and_turned<KIND>(x, norm.eps, w, bias, angles, y);
+        normed_and_turned(x, KIND, norm.eps, w, bias, angles, y);
         LaneRow<T, D, HALVES>::store(a.out[z].row(b, h, n), L, y);
     }
 }
@@ -324,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(GradArgs<T> a,
         next_dy.load(a.dy[z].row(b, h0, n), L);
         LaneTurn angles;
         turn_of_token(t, L, n, angles);
-        float w[8];
+            float w[8];
         load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
         for (int h = h0; h < h1; ++h) {
             const Lane x = next_x, dy = next_dy;
@@ -340,12 +350,14 @@ __global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(GradArgs<T> a,
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dx[e] = g[e];
             } else {
-                double mean, r;
-                row_norm<KIND>(x, norm.eps, mean, r);
+                double u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = (double)x[e];
+                const double r = row_norm<D>(u, KIND, norm.eps);
                 float xhat[8], mv = 0.0f, mvh = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    xhat[e] = (float)(((double)x[e] - mean) * r);
+                    xhat[e] = (float)(u[e] * r);
                     dw[e] = fmaf(g[e], xhat[e], dw[e]);
                     db[e] += g[e];
                     const float v = g[e] * w[e];
@@ -444,8 +456,7 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x
     typedef LaneRow<float, D, HALVES> Lane;
     const int first = Lane::first(L), second = first + Lane::SECOND;
     if constexpr (BITS == 16) {
-        const unsigned v[4] = {f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16, f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16,
-                               f32_to_bf16_bits(x[4]) | f32_to_bf16_bits(x[5]) << 16, f32_to_bf16_bits(x[6]) | f32_to_bf16_bits(x[7]) << 16};
+        const unsigned v[4] = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
         if constexpr (HALVES) {
             *(uint2v*)(row + 2 * first) = (uint2v){v[0], v[1]};
             *(uint2v*)(row + 2 * second) = (uint2v){v[2], v[3]};
@@ -500,134 +511,228 @@ __device__ __forceinline__ void stage_codes(uint8_t* stage, int token, int L, co
     }
 }
 
-// The staged tile to memory, by THREADS threads, 16 bytes (4-bit codes: 4) each in turn.
-template <int BITS, int BLK, int D, int THREADS>
+// The staged tile to memory, by the workgroup, 16 bytes (4-bit codes: 4) each in turn.
+template <int BITS, int BLK, int D>
 __device__ __forceinline__ void store_staged(uint8_t* out, const uint8_t* stage, int tid) {
     constexpr int ELEMS = BLK * D, SSTR = stage_row<BITS, BLK>();
     if constexpr (BITS == 4) {
         // 8 consecutive slots of one channel -> 4 bytes: byte t = slot t | slot 4+t << 4
         constexpr int GROUPS = ELEMS / 8;
-        for (int g = tid; g < GROUPS; g += THREADS) {
+        for (int g = tid; g < GROUPS; g += kThreads) {
             const unsigned* src = (const unsigned*)(stage + (g / (BLK / 8)) * SSTR + (g % (BLK / 8)) * 8);
             *(unsigned*)(out + (size_t)g * 4) = (src[0] & 0x0f0f0f0fu) | ((src[1] & 0x0f0f0f0fu) << 4);
         }
     } else if constexpr (BITS == 8) {
         constexpr int VEC = ELEMS / 16;
-        for (int v = tid; v < VEC; v += THREADS) {
+        for (int v = tid; v < VEC; v += kThreads) {
             const unsigned* src = (const unsigned*)(stage + (v / (BLK / 16)) * SSTR + (v % (BLK / 16)) * 16);
             ((uint4*)out)[v] = make_uint4(src[0], src[1], src[2], src[3]);
         }
     } else {
         constexpr int VEC = ELEMS / 8;
-        for (int v = tid; v < VEC; v += THREADS) ((uint4*)out)[v] = ((const uint4*)stage)[v];
+        for (int v = tid; v < VEC; v += kThreads) ((uint4*)out)[v] = ((const uint4*)stage)[v];
     }
 }
 
 // ---- with reorder and quantizer ------------------------------------------------------------------------------------
+// The six axis orders, as the kernels below use them.
+struct Orders {
+    uint32_t ids[kMaxHeads / 4];  // a head's order id, a byte each
+    int extent[6][2];             // of the middle and of the fastest axis
+    int stride[6][3];             // default-order strides of the slowest, middle and fastest axis
+    int place[6][3];              // which of the three the frame, height and width axis is
+    double inv[6][2];             // 1 / extent
+};
+
 template <typename T>
 struct QuantArgs {
     Rows<const T> in[3];
     uint8_t* codes[3];
     float* scales[3];
-    int n_tokens, kblocks, nh, kind;
-    double inv[6][2];  // per axis order: 1 / extent of the middle and of the fastest axis
-    ReorderTable table;
+    int n_tokens, kblocks, nh, kind, span;  // blocks per workgroup
+    Orders orders;
 };
 
-// Position in default order, and the grid coordinates, of the token at n_new of the head's sequence.
-struct Source {
-    int n, f, h, w;
+// A head's order, and where a token of its sequence comes from.
+struct HeadOrder {
+    int e1, e2, s0, s1, s2, place0, place1, place2;
+    double i1, i2;
+    __device__ __forceinline__ HeadOrder(const Orders& o, int h) {
+        const int id = o.ids[h >> 2] >> 8 * (h & 3) & 255;
+        e1 = o.extent[id][0], e2 = o.extent[id][1], s0 = o.stride[id][0], s1 = o.stride[id][1], s2 = o.stride[id][2];
+        i1 = o.inv[id][0], i2 = o.inv[id][1];
+        place0 = o.place[id][0], place1 = o.place[id][1], place2 = o.place[id][2];
+    }
+    // The coordinates along the order's axes of the image token at n_new; returns its position in default order.  Factors are below 2^24, or
+    // are 2^24 (an extent or a stride of all tokens) beside a 0.
+    __device__ __forceinline__ int source(int n_new, int& c0, int& c1, int& c2) const {
+        const int q = quotient_of(n_new, i2);
+        c2 = n_new - __umul24(q, e2);
+        c0 = quotient_of(q, i1);
+        c1 = q - __umul24(c0, e1);
+        return __umul24(c0, s0) + __umul24(c1, s1) + __umul24(c2, s2);
+    }
 };
-template <typename T>
-__device__ __forceinline__ Source source_of(const QuantArgs<T>& a, const Turning& t, int order, int n_new) {
-    if (n_new >= t.n_img) return {n_new, 0, 0, 0};
-    const int* fwd = a.table.fwd[order];
-    const int q = quotient_of(n_new, a.inv[order][1]), c2 = n_new - q * fwd[1], c0 = quotient_of(q, a.inv[order][0]), c1 = q - c0 * fwd[0];
-    const AxisOrder axes = axis_order(order);
-    return {c0 * fwd[2] + c1 * fwd[3] + c2 * fwd[4], axes.a[0] == 0 ? c0 : axes.a[1] == 0 ? c1 : c2, axes.a[0] == 1 ? c0 : axes.a[1] == 1 ? c1 : c2,
-            axes.a[0] == 2 ? c0 : axes.a[1] == 2 ? c1 : c2};
-}
 
-// One workgroup owns one group of one tensor (grid: blocks, batches x heads, Q K V); the tile stays in registers between the pass for
-// the largest value and the codes.
-template <typename T, int BLK, int D, int BITS, int LAYOUT, bool HALVES>
+// by value: a conditional between members would choose between their addresses, and load from there
+__device__ __forceinline__ int pick(int c0, int c1, int c2, int place) { return place == 0 ? c0 : place == 1 ? c1 : c2; }
+
+// Where a lane's angles lie in the table when its four pairs belong to one axis (Turning::fours).
+struct LaneAxis {
+    int place, pairs, base;  // base < 0: the lane's pairs do not turn
+    __device__ __forceinline__ LaneAxis(const Turning& t, const HeadOrder& o, int L) {
+        const int to1 = t.pairs[0], to2 = to1 + t.pairs[1], p0 = 4 * L, a = p0 < to1 ? 0 : p0 < to2 ? 1 : 2;
+        place = pick(o.place0, o.place1, o.place2, a);
+        pairs = pick(t.pairs[0], t.pairs[1], t.pairs[2], a);
+        base = p0 >= t.total ? -1 : pick(t.base[0], t.base[1] - to1, t.base[2] - to2, a) + p0;
+    }
+};
+
+
+// Q or K: one workgroup goes through `span` blocks of a head and reads a block while it works on the one before; the block stays in registers between
+// the pass for the largest value and the codes.
+template <typename T, int BLK, int D, int BITS, bool HALVES, bool FOURS>
 __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turning& t, const Norms& norm, int z) {
-    constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8;
+    constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
     constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
-    __shared__ __attribute__((aligned(16))) uint8_t stage[LAYOUT == PARO_VT ? stage_bytes<BITS, BLK, D>() : 16];
-    __shared__ float wave_amax[kThreads / 64];
-    const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, blk = blockIdx.x, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
-    const size_t group = (size_t)bh * a.kblocks + blk;
-    const int order = a.table.perm[h];
-    LaneRow<T, D, HALVES> x[IT];
-    Source from[IT];
+    __shared__ float wave_amax[2][WAVES];
+    const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
+    const int blk0 = blockIdx.x * a.span, blk1 = min(blk0 + a.span, a.kblocks);
+    const HeadOrder order(a.orders, h);
+    const LaneAxis axis(t, order, L);
+    const T* base = a.in[z].row(b, h, 0) + LaneRow<T, D, HALVES>::first(L);
+    const int stride = a.in[z].token;
+    LaneRow<T, D, HALVES> next[IT];
+    int next_at[IT];  // FOURS: where the row's angles lie in the table, < 0: it does not turn; else the token
+    const auto read = [&](int blk) {
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-        const int n_new = blk * BLK + it * ROWS + row;
-        if (n_new < a.n_tokens) {
-            from[it] = source_of(a, t, order, n_new);
-            x[it].load(a.in[z].row(b, h, from[it].n), L);
+        for (int it = 0; it < IT; ++it) {
+            const int n_new = blk * BLK + it * ROWS + row;
+            int c0, c1, c2, n = order.source(min(n_new, t.n_img - 1), c0, c1, c2);
+            const bool image = n_new < t.n_img;
+            if (!image) n = min(n_new, a.n_tokens - 1);
+            next[it].load(base + (int64_t)n * stride, 0);
+            if constexpr (FOURS) next_at[it] = image && axis.base >= 0 ? axis.base + __umul24(pick(c0, c1, c2, axis.place), axis.pairs) : -1;
+            else next_at[it] = n;
         }
-    }
-    float y[IT][8], amax = 0.0f;
+    };
+    read(blk0);
+    float w[8], bias[8];
+    const auto vectors = [&](bool text) {
+        load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
+        load_vector<D, HALVES>(norm.b[z][text], L, -0.0f, bias);
+    };
+    bool text_vectors = blk0 * BLK >= t.n_img;
+    vectors(text_vectors);
+    for (int blk = blk0; blk < blk1; ++blk) {
+        LaneRow<T, D, HALVES> x[IT];
+        LaneTurn turn[IT];
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-        const int n_new = blk * BLK + it * ROWS + row;
-        if (n_new < a.n_tokens) {
-            if constexpr (LAYOUT == PARO_VT) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[it][e] = x[it][e];
+        for (int it = 0; it < IT; ++it) {
+            x[it] = next[it];
+            LaneTurn& r = turn[it];
+            if constexpr (FOURS) {
+                r.turned = next_at[it] >= 0 ? 15 : 0;
+                const float4* v = (const float4*)(t.table + 2 * (int64_t)max(next_at[it], 0));
+                const float4 p = v[0], q = v[1];
+                r.c[0] = p.x, r.s[0] = p.y, r.c[1] = p.z, r.s[1] = p.w, r.c[2] = q.x, r.s[2] = q.y, r.c[3] = q.z, r.s[3] = q.w;
             } else {
-                const int text = n_new >= t.n_img;
-                LaneTurn angles;
-                if (!text && t.total) load_turn(t, L, from[it].f, from[it].h, from[it].w, angles);
-                else angles.none();
-                float w[8], bias[8];
-                if (a.kind == PARO_NORM_NONE) {
-                    normed_and_turned<PARO_NORM_NONE>(x[it], norm.eps, w, bias, angles, y[it]);
-                } else {
-                    load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
-                    if (a.kind == PARO_NORM_RMS) {
-                        normed_and_turned<PARO_NORM_RMS>(x[it], norm.eps, w, bias, angles, y[it]);
-                    } else {
-                        load_vector<D, HALVES>(norm.b[z][text], L, 0.0f, bias);
-                        normed_and_turned<PARO_NORM_LAYER>(x[it], norm.eps, w, bias, angles, y[it]);
-                    }
-                }
+                turn_of_token(t, L, next_at[it], r);
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[it][e] = 0.0f;
         }
+        if (blk + 1 < blk1) read(blk + 1);
+        const size_t group = (size_t)bh * a.kblocks + blk;
+        // a block's rows are image tokens, text tokens or both
+        const bool mixed = blk * BLK < t.n_img && blk * BLK + BLK > t.n_img;
+        if (!text_vectors && blk * BLK >= t.n_img) vectors(text_vectors = true);
+        float y[IT][8], amax = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e]));
-    }
-    float scale = 1.0f;
-    if constexpr (BITS != 16) {
-        amax = wave_max(amax);
-        if ((tid & 63) == 0) wave_amax[tid >> 6] = amax;
-        __syncthreads();
-        amax = fmaxf(fmaxf(wave_amax[0], wave_amax[1]), fmaxf(wave_amax[2], wave_amax[3]));
-        if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
-    }
-    if (tid == 0) a.scales[z][group] = scale;
-    const GroupDivider quotient(scale);
-    uint8_t* out = a.codes[z] + group * OUT_BYTES;
+        for (int it = 0; it < IT; ++it) {
+            const int n_new = blk * BLK + it * ROWS + row;
+            if (mixed) vectors(n_new >= t.n_img);
+            normed_and_turned(x[it], a.kind, norm.eps, w, bias, turn[it], y[it]);
+            if (n_new >= a.n_tokens) {
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-        if constexpr (LAYOUT == PARO_ROWS) store_codes<BITS, D, HALVES>(out + (it * ROWS + row) * (D * BITS / 8), L, y[it], quotient);
-        else stage_codes<BITS, BLK, D, HALVES>(stage, it * ROWS + row, L, y[it], quotient);
-    }
-    if constexpr (LAYOUT == PARO_VT) {
-        __syncthreads();
-        store_staged<BITS, BLK, D, kThreads>(out, stage, tid);
+                for (int e = 0; e < 8; ++e) y[it][e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e]));
+        }
+        if (mixed) text_vectors = false, vectors(false);
+        float scale = 1.0f;
+        if constexpr (BITS != 16) {
+            amax = wave_max(amax);
+            float* meet = wave_amax[blk & 1];  // the block before last has been read by everyone who is past the last one's barrier
+            if ((tid & 63) == 0) meet[tid >> 6] = amax;
+            __syncthreads();
+#pragma unroll
+            for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, meet[wave]);
+            if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
+        }
+        if (tid == 0) a.scales[z][group] = scale;
+        const GroupDivider quotient(scale);
+        uint8_t* out = a.codes[z] + group * OUT_BYTES;
+#pragma unroll
+        for (int it = 0; it < IT; ++it) store_codes<BITS, D, HALVES>(out + (it * ROWS + row) * (D * BITS / 8), L, y[it], quotient);
     }
 }
 
-template <typename T, int BLK, int D, int QKBITS, int PVBITS, bool HALVES>
+// V: a block's codes are transposed through LDS.
+template <typename T, int BLK, int D, int BITS>
+__device__ __forceinline__ void quantize_transposed(const QuantArgs<T>& a, const Turning& t) {
+    constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
+    constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
+    __shared__ __attribute__((aligned(16))) uint8_t stage[stage_bytes<BITS, BLK, D>()];
+    __shared__ float wave_amax[WAVES];
+    const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
+    const int blk0 = blockIdx.x * a.span, blk1 = min(blk0 + a.span, a.kblocks);
+    const HeadOrder order(a.orders, h);
+    const T* base = a.in[2].row(b, h, 0);
+    const int stride = a.in[2].token;
+    LaneRow<T, D, false> next[IT];
+    const auto read = [&](int blk) {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int n_new = blk * BLK + it * ROWS + row;
+            int c0, c1, c2, n = order.source(min(n_new, t.n_img - 1), c0, c1, c2);
+            if (n_new >= t.n_img) n = min(n_new, a.n_tokens - 1);
+            next[it].load(base + (int64_t)n * stride, L);
+            if (n_new >= a.n_tokens) next[it].zero();
+        }
+    };
+    read(blk0);
+    for (int blk = blk0; blk < blk1; ++blk) {
+        const size_t group = (size_t)bh * a.kblocks + blk;
+        float y[IT][8], amax = 0.0f;
+#pragma unroll
+        for (int it = 0; it < IT; ++it)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e] = next[it][e]));
+        if (blk + 1 < blk1) read(blk + 1);
+        float scale = 1.0f;
+        if constexpr (BITS != 16) {
+            amax = wave_max(amax);
+            if ((tid & 63) == 0) wave_amax[tid >> 6] = amax;
+            __syncthreads();
+#pragma unroll
+            for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, wave_amax[wave]);
+            if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
+        } else {
+            __syncthreads();
+        }
+        if (tid == 0) a.scales[2][group] = scale;
+        const GroupDivider quotient(scale);
+#pragma unroll
+        for (int it = 0; it < IT; ++it) stage_codes<BITS, BLK, D, false>(stage, it * ROWS + row, L, y[it], quotient);
+        __syncthreads();
+        store_staged<BITS, BLK, D>(a.codes[2] + group * OUT_BYTES, stage, tid);
+    }
+}
+
+template <typename T, int BLK, int D, int QKBITS, int PVBITS, bool HALVES, bool FOURS>
 __global__ __launch_bounds__(kThreads) void norm_rope_quantize_kernel(QuantArgs<T> a, Turning t, Norms norm) {
-    if (blockIdx.z < 2) quantize_rows<T, BLK, D, QKBITS, PARO_ROWS, HALVES>(a, t, norm, blockIdx.z);
-    else quantize_rows<T, BLK, D, PVBITS, PARO_VT, false>(a, t, norm, 2);
+    if (blockIdx.z < 2) quantize_rows<T, BLK, D, QKBITS, HALVES, FOURS>(a, t, norm, blockIdx.z);
+    else quantize_transposed<T, BLK, D, PVBITS>(a, t);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -643,6 +748,7 @@ static int check_rows(const paro_shape* s, int64_t n, paro_dtype dtype, const pa
         if (extent[i] == 1) continue;
         if (stride[i] < 0 || stride[i] > ((int64_t)1 << 56) / extent[i])
             return fail(PARO_EINVAL, "%s: a stride of %lld elements is negative or out of range", what, (long long)stride[i]);
+        if (i == 2 && stride[i] > INT32_MAX) return fail(PARO_EUNSUPPORTED, "%s: a token stride of %lld elements exceeds 2^31", what, (long long)stride[i]);
         if (stride[i] * size % 16) return fail(PARO_EINVAL, "%s: a stride of %lld elements is no multiple of 16 bytes", what, (long long)stride[i]);
     }
     if (!written) return PARO_OK;
@@ -705,7 +811,7 @@ static int make_norms(const paro_qk_norm* norm, Norms* out) {
 }
 
 template <typename T>
-static Rows<T> rows_of(const paro_strided* r) { return {(T*)r->data, r->batch, r->head, r->token}; }
+static Rows<T> rows_of(const paro_strided* r) { return {(T*)r->data, r->batch, r->head, (int)r->token}; }
 
 // Heads that a workgroup goes through: so few that there are `least` workgroups (below that a launch lasts as long as a workgroup), and
 // not more than three while there are fewer than `enough`.
@@ -811,11 +917,11 @@ static void launch_grad(const paro_shape* s, int64_t n, paro_dtype dtype, int ki
     });
 }
 
-template <typename T, int BLK, int D, bool HALVES>
+template <typename T, int BLK, int D, bool HALVES, bool FOURS>
 static bool launch_quant_bits(int bits_qk, int bits_pv, dim3 grid, hipStream_t st, const QuantArgs<T>& a, const Turning& t, const Norms& norm) {
 #define PARO_QKV_CASE(QK, PV)                                                                                                             \
     if (bits_qk == QK && bits_pv == PV) {                                                                                                 \
-        hipLaunchKernelGGL((norm_rope_quantize_kernel<T, BLK, D, QK, PV, HALVES>), grid, dim3(kThreads), 0, st, a, t, norm);            \
+        hipLaunchKernelGGL((norm_rope_quantize_kernel<T, BLK, D, QK, PV, HALVES, FOURS>), grid, dim3(kThreads), 0, st, a, t, norm); \
         return true;                                                                                                                      \
     }
     PARO_QKV_CASE(8, 8)
@@ -827,21 +933,32 @@ static bool launch_quant_bits(int bits_qk, int bits_pv, dim3 grid, hipStream_t s
     return false;
 }
 
-template <typename T, bool HALVES>
+template <typename T, bool HALVES, bool FOURS>
 static bool launch_quant(const paro_shape* s, int bits_qk, int bits_pv, dim3 grid, hipStream_t st, const QuantArgs<T>& a, const Turning& t, const Norms& norm) {
-    if (s->block == 64 && s->d == 64) return launch_quant_bits<T, 64, 64, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
-    if (s->block == 64) return launch_quant_bits<T, 64, 128, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
-    if (s->d == 64) return launch_quant_bits<T, 32, 64, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
-    return launch_quant_bits<T, 32, 128, HALVES>(bits_qk, bits_pv, grid, st, a, t, norm);
+    if (s->block == 64 && s->d == 64) return launch_quant_bits<T, 64, 64, HALVES, FOURS>(bits_qk, bits_pv, grid, st, a, t, norm);
+    if (s->block == 64) return launch_quant_bits<T, 64, 128, HALVES, FOURS>(bits_qk, bits_pv, grid, st, a, t, norm);
+    if (s->d == 64) return launch_quant_bits<T, 32, 64, HALVES, FOURS>(bits_qk, bits_pv, grid, st, a, t, norm);
+    return launch_quant_bits<T, 32, 128, HALVES, FOURS>(bits_qk, bits_pv, grid, st, a, t, norm);
 }
 
 template <typename T>
 static int quantize_entry(const paro_shape* s, int64_t n, int64_t kb, int kind, int pairs, int bits_qk, int bits_pv, const uint8_t* h_perm_ids, const paro_strided* const (&in)[3],
                           void* const (&codes)[3], float* const (&scales)[3], const Turning& t, const Norms& norm, hipStream_t st) {
     QuantArgs<T> a;
-    if (int e = make_reorder_table(s, h_perm_ids, &a.table)) return e;
-    for (int p = 0; p < 6; ++p)
-        for (int i = 0; i < 2; ++i) a.inv[p][i] = 1.0 / a.table.fwd[p][i];
+    ReorderTable table;
+    if (int e = make_reorder_table(s, h_perm_ids, &table)) return e;
+    memset(&a.orders, 0, sizeof(a.orders));
+    for (int h = 0; h < s->nh; ++h) a.orders.ids[h >> 2] |= (uint32_t)table.perm[h] << 8 * (h & 3);
+    for (int p = 0; p < 6; ++p) {
+        for (int i = 0; i < 2; ++i) {
+            a.orders.extent[p][i] = table.fwd[p][i];
+            a.orders.inv[p][i] = 1.0 / table.fwd[p][i];
+        }
+        for (int i = 0; i < 3; ++i) {
+            a.orders.stride[p][i] = table.fwd[p][2 + i];
+            a.orders.place[p][axis_order(p).a[i]] = i;
+        }
+    }
     for (int i = 0; i < 3; ++i) {
         a.in[i] = rows_of<const T>(in[i]);
         a.codes[i] = (uint8_t*)codes[i];
@@ -851,8 +968,11 @@ static int quantize_entry(const paro_shape* s, int64_t n, int64_t kb, int kind, 
     a.kblocks = (int)kb;
     a.nh = s->nh;
     a.kind = kind;
-    const auto run = pairs == PARO_PAIRS_HALVES ? launch_quant<T, true> : launch_quant<T, false>;
-    if (!run(s, bits_qk, bits_pv, dim3((unsigned)kb, (unsigned)(s->B * s->nh), 3), st, a, t, norm))
+    a.span = 1;
+    while (a.span < 8 && 3 * (int64_t)s->B * s->nh * ((kb + a.span) / (a.span + 1)) >= 4096) ++a.span;
+    const auto run = pairs == PARO_PAIRS_HALVES ? (t.fours ? launch_quant<T, true, true> : launch_quant<T, true, false>)
+                                                : (t.fours ? launch_quant<T, false, true> : launch_quant<T, false, false>);
+    if (!run(s, bits_qk, bits_pv, dim3((unsigned)((kb + a.span - 1) / a.span), (unsigned)(s->B * s->nh), 3), st, a, t, norm))
         return fail(PARO_EINVAL, "bits (qk=%d, pv=%d): expected (8,8), (8,4), (4,4), (4,8) or (16,16)", bits_qk, bits_pv);
     return check_launch("paro_qk_norm_rope_quantize_qkv");
 }

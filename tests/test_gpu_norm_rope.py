@@ -299,6 +299,26 @@ def test_quantize(case, dtype, bits):
         assert np.array_equal(gs[0][0, h].cpu().numpy(), scales) and np.array_equal(got[0][0, h].cpu().numpy(), codes), h
 
 
+@pytest.mark.parametrize("case", [dict(d=64, kind="layer", layout="fused"), dict(d=128, kind="rms", halves=1, dims=(44, 42, 42)), dict(d=64, kind="none", block=32)], ids=_id)
+def test_quantize_many_blocks(case):
+    """Workgroups that go through several blocks, from image tokens into text: the codes and scales of the two calls."""
+    import torch
+
+    pb = _pb()
+    for bits in ((8, 8), (16, 16)):
+        p = Problem(B=2, nh=48, grid=(2, 9, 125), T=200, text_norm=case["kind"] != "none", dtype="float32", **case)
+        assert 3 * 2 * 48 * ((pb.paro_nblocks(p.s) + 1) // 2) >= 4096  # two blocks or more each
+        ids = (np.arange(48) % 6).astype(np.uint8)
+        got, gs = _buffers(pb, p.s, *bits, 2)
+        pb.paro_qk_norm_rope_quantize_qkv(p.s, *bits, ids, p.axes, p.table, p.norm, *p.x, got[0], gs[0], got[1], gs[1], got[2], gs[2])
+        y = [torch.empty((2, 48, p.n, p.d), device="cuda:0") for _ in range(2)]
+        pb.paro_qk_norm_rope(p.s, p.axes, p.table, p.norm, p.x[0], p.x[1], *y)
+        want, ws = _buffers(pb, p.s, *bits, 1)
+        pb.paro_permute_quantize_qkv(p.s, *bits, ids, *y, p.x[2].contiguous(), want[0], ws[0], want[1], ws[1], want[2], ws[2])
+        for i in range(3):
+            assert torch.equal(got[i], want[i]) and torch.equal(gs[i], ws[i]), i
+
+
 def test_a_layer_from_projections_to_attention():
     """ParoAttention on Q, K, V as a projection leaves them: the bits of norms and rotation, then the fused layer."""
     import torch

@@ -102,7 +102,7 @@ COMMON = {
     "odd channels": _set(("axes", "dims", 0), 15), "more channels than a row": _set(("axes", "dims", 2), 26), "no way to pair": _set(("axes", "pairs"), 7),
     "a type": _set(("dtype",), 2), "no table": _set(("table",), None), "a table off its bytes": _set(("table",), at(50, 8)),
     "no input": _set(("rows", 0), None), "an input's null": _set(("rows", 0, "data"), None), "an input off its bytes": _set(("rows", 0, "data"), at(0, 8)),
-    "a negative stride": _set(("rows", 0, "token"), -64), "a stride off its bytes": _set(("rows", 0, "token"), 68), "a stride beyond all memory": _set(("rows", 0, "batch"), 1 << 60),
+    "a negative stride": _set(("rows", 0, "token"), -64), "a stride off its bytes": _set(("rows", 0, "token"), 68), "a stride beyond all memory": _set(("rows", 0, "batch"), 1 << 60), "a token stride of 2^31": _set(("rows", 0, "token"), 1 << 31),
 }
 
 
