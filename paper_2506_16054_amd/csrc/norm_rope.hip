@@ -156,14 +156,12 @@ __device__ __forceinline__ float rows_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// 1 / sqrt(v): the instruction's estimate and two Newton steps, y <- y + y (1/2 - v/2 y^2), which square its relative error.  The
-// estimate stands where v is 0 or infinite.
+// 1 / sqrt(v): the instruction's estimate y and one step of third order, y (1 + e/2 + 3/8 e^2) with e = 1 - v y^2, which leaves 5/16 e^3 of its
+// relative error (below 2^-20, hence 2^-60).  The estimate stands where v is 0 or infinite.
 __device__ __forceinline__ double rsqrt_of(double v) {
-    const double y0 = __builtin_amdgcn_rsq(v);
-    double y = y0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) y = fma(y, fma(-0.5 * v * y, y, 0.5), y);
-    return v > 0.0 && v < __builtin_inf() ? y : y0;
+    const double y = __builtin_amdgcn_rsq(v), e = fma(-v * y, y, 1.0);
+    const double better = fma(y * e, fma(e, 0.375, 0.5), y);
+    return __builtin_amdgcn_class(v, 0x264) ? y : better;  // zeros and infinities
 }
 
 // What a row is divided by; under PARO_NORM_LAYER its values lose their mean first.
@@ -250,9 +248,9 @@ __device__ __forceinline__ void turn_lane(V (&u)[8], const LaneTurn& t) {
 }
 
 // The row behind norm and rotation, rounded to binary32.  w and b: 1 and -0 where there is nothing (exact, signs of zeros included).
-template <typename T, int D, bool HALVES>
-__device__ __forceinline__ void normed_and_turned(const LaneRow<T, D, HALVES>& x, int kind, double eps, const float (&w)[8], const float (&b)[8],
-                                                  const LaneTurn& t, float (&y)[8]) {
+template <typename T, int D, bool HALVES, typename W>
+__device__ __forceinline__ void normed_and_turned(const LaneRow<T, D, HALVES>& x, int kind, double eps, const W& w, const W& b, const LaneTurn& t,
+                                                  float (&y)[8]) {
     double u[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] = (double)x[e];
@@ -433,21 +431,43 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(const float* __restrict
 }
 
 // ---- codes of a tile in registers ----------------------------------------------------------------------------------
-// Rows of the staged transposed tile (one channel each) are 4 bytes longer than the block for the integer codes, so that the
-// byte stores of lanes that hold one token's channels fall into different LDS banks; bf16 takes 16-bit words.
+// Rows of the staged transposed tile (one channel each) are 4 bytes longer than the block, so that the stores of lanes that hold one token's
+// channels fall into different LDS banks (bf16, 24 heads of 4608 tokens, d = 128: 44 -> 38 us); bf16 takes 16-bit words.
 template <int BITS, int BLK>
-constexpr int stage_row() { return BITS == 16 ? BLK : BLK + 4; }
+constexpr int stage_row() { return BITS == 16 ? BLK + 2 : BLK + 4; }
 template <int BITS, int BLK, int D>
 constexpr int stage_bytes() { return D * stage_row<BITS, BLK>() * (BITS == 16 ? 2 : 1); }
+
+// The largest of a value over a wavefront, in every lane: as row_sum and rows_sum.
+__device__ __forceinline__ float wavefront_max(float v) {
+    v = fmaxf(v, moved<0xB1>(v));
+    v = fmaxf(v, moved<0x4E>(v));
+    v = fmaxf(v, moved<0x141>(v));
+    v = fmaxf(v, moved<0x140>(v));
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
 
 template <int BITS>
 __device__ __forceinline__ void codes_of(const float (&x)[8], const GroupDivider& quotient, int (&q)[8]) {
     constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
+    float r[8];
+    if (quotient.generic) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float r = rintf(quotient(x[e]));  // v_rndne_f32: round half to even
-        q[e] = (int)fminf(fmaxf(r, -QMAX), QMAX);
+        for (int e = 0; e < 8; ++e) r[e] = x[e] / quotient.scale;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q0 = x[e] * quotient.inv;
+            r[e] = fmaf(fmaf(-q0, quotient.scale, x[e]), quotient.inv, q0);
+        }
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = (int)fminf(fmaxf(rintf(r[e]), -QMAX), QMAX);  // v_rndne_f32: round half to even
 }
 
 // PARO_ROWS: a lane's codes into its row of the group.
@@ -522,15 +542,12 @@ __device__ __forceinline__ void store_staged(uint8_t* out, const uint8_t* stage,
             const unsigned* src = (const unsigned*)(stage + (g / (BLK / 8)) * SSTR + (g % (BLK / 8)) * 8);
             *(unsigned*)(out + (size_t)g * 4) = (src[0] & 0x0f0f0f0fu) | ((src[1] & 0x0f0f0f0fu) << 4);
         }
-    } else if constexpr (BITS == 8) {
-        constexpr int VEC = ELEMS / 16;
-        for (int v = tid; v < VEC; v += kThreads) {
-            const unsigned* src = (const unsigned*)(stage + (v / (BLK / 16)) * SSTR + (v % (BLK / 16)) * 16);
+    } else {
+        constexpr int BYTES = BITS / 8, PIECES = BLK * BYTES / 16;  // 16-byte pieces per channel
+        for (int v = tid; v < D * PIECES; v += kThreads) {
+            const unsigned* src = (const unsigned*)(stage + (v / PIECES) * SSTR * BYTES + (v % PIECES) * 16);
             ((uint4*)out)[v] = make_uint4(src[0], src[1], src[2], src[3]);
         }
-    } else {
-        constexpr int VEC = ELEMS / 8;
-        for (int v = tid; v < VEC; v += kThreads) ((uint4*)out)[v] = ((const uint4*)stage)[v];
     }
 }
 
@@ -589,41 +606,95 @@ struct LaneAxis {
 };
 
 
-// Q or K: one workgroup goes through `span` blocks of a head and reads a block while it works on the one before; the block stays in registers between
-// the pass for the largest value and the codes.
+// Where the rows of a workgroup's blocks come from, in LDS: position in default order and the coordinates along the order's axes (the first -1
+// for a token that does not turn).  A row has 8 or 16 lanes; one thread finds its place for all of them.
+constexpr int kSpan = 8;  // blocks per workgroup at most
+template <int BLK>
+struct Places {
+    int4 row[kSpan * BLK];
+    template <typename T>
+    __device__ __forceinline__ void fill(const QuantArgs<T>& a, const Turning& t, const HeadOrder& order, int blk0, int blocks) {
+        for (int i = threadIdx.x; i < blocks * BLK; i += kThreads) {
+            const int n_new = blk0 * BLK + i;
+            int4 p;
+            p.x = order.source(min(n_new, t.n_img - 1), p.y, p.z, p.w);
+            if (n_new >= t.n_img) p.x = min(n_new, a.n_tokens - 1), p.y = -1;
+            row[i] = p;
+        }
+    }
+};
+
+// Weights and biases of a tensor as binary64 in LDS, of image and of text tokens: a row's lanes read those of their channels without a conversion and
+// without registers that hold them.  Pair i of all lanes lies in one piece, so that a read of 16 bytes per lane meets no bank twice.
+template <int D, bool HALVES>
+struct Vectors {
+    double v[2][2][D];  // [text][weight, bias][pair of a lane][lane][2]
+    static constexpr int LANES = D / 8;
+    __device__ __forceinline__ void fill(const Norms& norm, int z) {
+#pragma unroll
+        for (int j = 0; j < 4 * D / kThreads; ++j) {
+            // a wavefront fills one vector (or half of one): which is a scalar, and so is its address
+            const int which = __builtin_amdgcn_readfirstlane((threadIdx.x + j * kThreads) / D), c = threadIdx.x % D, bias = which & 1, text = which >> 1;
+            const float* p = bias ? norm.b[z][text] : norm.w[z][text];
+            const int L = HALVES ? c % (D / 2) / 4 : c / 8, e = HALVES ? c % 4 + (c >= D / 2 ? 4 : 0) : c % 8;
+            v[text][bias][((e >> 1) * LANES + L) * 2 + (e & 1)] = p ? (double)p[c] : bias ? -0.0 : 1.0;
+        }
+    }
+};
+// A lane's eight of them.
+template <int D>
+struct LaneVector {
+    const double* p;  // behind the lane's first two
+    __device__ __forceinline__ double operator[](int e) const { return p[(e >> 1) * (D / 8) * 2 + (e & 1)]; }
+};
+
+// What a workgroup holds in LDS: for Q and K, and for V.
+template <int BLK, int D, bool HALVES>
+struct RowsLds {
+    Places<BLK> places;
+    Vectors<D, HALVES> vectors;
+    float amax[2][kThreads / 64];
+};
+template <int BLK, int D, int BITS>
+struct TransposedLds {
+    Places<BLK> places;
+    __attribute__((aligned(16))) uint8_t stage[stage_bytes<BITS, BLK, D>()];
+    float amax[kThreads / 64];
+};
+
+// Q (z = 0) or K: one workgroup goes through `span` blocks of a head and reads a block while it works on the one before; the block stays in
+// registers between the pass for the largest value and the codes.
+//
+// Bound by vector instructions with 8-bit codes (some 200 for the eight channels of a lane, a third of them binary64), by HBM with bf16.
+// 48 heads of 17550 bf16 tokens, d = 64, layer norms, out of one projection's output: 123 us with 8-bit codes (485 MB), 135 with bf16 (647 MB, 4.8 TB/s); one
+// block per workgroup, no reading ahead, each row's place found by all of its lanes, weights in registers: 192 and 190.  Q and K in one
+// workgroup, for their common places and angles: 6 % more registers, slower by 3 %.
 template <typename T, int BLK, int D, int BITS, bool HALVES, bool FOURS>
-__device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turning& t, const Norms& norm, int z) {
+__device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turning& t, const Norms& norm, int z, uint8_t* lds) {
     constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
     constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
-    __shared__ float wave_amax[2][WAVES];
+    RowsLds<BLK, D, HALVES>& s = *(RowsLds<BLK, D, HALVES>*)lds;
     const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
     const int blk0 = blockIdx.x * a.span, blk1 = min(blk0 + a.span, a.kblocks);
     const HeadOrder order(a.orders, h);
     const LaneAxis axis(t, order, L);
-    const T* base = a.in[z].row(b, h, 0) + LaneRow<T, D, HALVES>::first(L);
+    const T* const base = a.in[z].row(b, h, 0);
     const int stride = a.in[z].token;
     LaneRow<T, D, HALVES> next[IT];
-    int next_at[IT];  // FOURS: where the row's angles lie in the table, < 0: it does not turn; else the token
+    int next_at[IT];  // FOURS: where the row's angles lie in the table, < 0: it does not turn
     const auto read = [&](int blk) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
-            const int n_new = blk * BLK + it * ROWS + row;
-            int c0, c1, c2, n = order.source(min(n_new, t.n_img - 1), c0, c1, c2);
-            const bool image = n_new < t.n_img;
-            if (!image) n = min(n_new, a.n_tokens - 1);
-            next[it].load(base + (int64_t)n * stride, 0);
-            if constexpr (FOURS) next_at[it] = image && axis.base >= 0 ? axis.base + __umul24(pick(c0, c1, c2, axis.place), axis.pairs) : -1;
-            else next_at[it] = n;
+            const int4 p = s.places.row[(blk - blk0) * BLK + it * ROWS + row];
+            next[it].load(base + (int64_t)p.x * stride, L);
+            if constexpr (FOURS) next_at[it] = (p.y | axis.base) >= 0 ? axis.base + (int)__umul24(pick(p.y, p.z, p.w, axis.place), axis.pairs) : -1;
         }
     };
+    s.places.fill(a, t, order, blk0, blk1 - blk0);
+    __syncthreads();
     read(blk0);
-    float w[8], bias[8];
-    const auto vectors = [&](bool text) {
-        load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
-        load_vector<D, HALVES>(norm.b[z][text], L, -0.0f, bias);
-    };
-    bool text_vectors = blk0 * BLK >= t.n_img;
-    vectors(text_vectors);
+    s.vectors.fill(norm, z);
+    __syncthreads();
     for (int blk = blk0; blk < blk1; ++blk) {
         LaneRow<T, D, HALVES> x[IT];
         LaneTurn turn[IT];
@@ -637,38 +708,37 @@ __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turni
                 const float4 p = v[0], q = v[1];
                 r.c[0] = p.x, r.s[0] = p.y, r.c[1] = p.z, r.s[1] = p.w, r.c[2] = q.x, r.s[2] = q.y, r.c[3] = q.z, r.s[3] = q.w;
             } else {
-                turn_of_token(t, L, next_at[it], r);
+                const int4 p = s.places.row[(blk - blk0) * BLK + it * ROWS + row];
+                if (p.y >= 0) load_turn(t, L, pick(p.y, p.z, p.w, order.place0), pick(p.y, p.z, p.w, order.place1), pick(p.y, p.z, p.w, order.place2), r);
+                else r.none();
             }
         }
         if (blk + 1 < blk1) read(blk + 1);
-        const size_t group = (size_t)bh * a.kblocks + blk;
-        // a block's rows are image tokens, text tokens or both
-        const bool mixed = blk * BLK < t.n_img && blk * BLK + BLK > t.n_img;
-        if (!text_vectors && blk * BLK >= t.n_img) vectors(text_vectors = true);
         float y[IT][8], amax = 0.0f;
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             const int n_new = blk * BLK + it * ROWS + row;
-            if (mixed) vectors(n_new >= t.n_img);
-            normed_and_turned(x[it], a.kind, norm.eps, w, bias, turn[it], y[it]);
+            const double* v = s.vectors.v[n_new >= t.n_img][0] + 2 * L;
+            normed_and_turned(x[it], a.kind, norm.eps, LaneVector<D>{v}, LaneVector<D>{v + D}, turn[it], y[it]);
             if (n_new >= a.n_tokens) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[it][e] = 0.0f;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e]));
+            for (int e = 0; e < 8; e += 2) amax = fmaxf(fmaxf(amax, fabsf(y[it][e])), fabsf(y[it][e + 1]));
         }
-        if (mixed) text_vectors = false, vectors(false);
         float scale = 1.0f;
         if constexpr (BITS != 16) {
-            amax = wave_max(amax);
-            float* meet = wave_amax[blk & 1];  // the block before last has been read by everyone who is past the last one's barrier
+            amax = wavefront_max(amax);
+            float* meet = s.amax[blk & 1];  // of two in turn: this one was read before the last block's barrier
             if ((tid & 63) == 0) meet[tid >> 6] = amax;
             __syncthreads();
 #pragma unroll
             for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, meet[wave]);
+            amax = uniform(amax);
             if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
         }
+        const size_t group = (size_t)bh * a.kblocks + blk;
         if (tid == 0) a.scales[z][group] = scale;
         const GroupDivider quotient(scale);
         uint8_t* out = a.codes[z] + group * OUT_BYTES;
@@ -679,60 +749,61 @@ __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turni
 
 // V: a block's codes are transposed through LDS.
 template <typename T, int BLK, int D, int BITS>
-__device__ __forceinline__ void quantize_transposed(const QuantArgs<T>& a, const Turning& t) {
+__device__ __forceinline__ void quantize_transposed(const QuantArgs<T>& a, const Turning& t, uint8_t* lds) {
     constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
     constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
-    __shared__ __attribute__((aligned(16))) uint8_t stage[stage_bytes<BITS, BLK, D>()];
-    __shared__ float wave_amax[WAVES];
+    TransposedLds<BLK, D, BITS>& s = *(TransposedLds<BLK, D, BITS>*)lds;
     const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
     const int blk0 = blockIdx.x * a.span, blk1 = min(blk0 + a.span, a.kblocks);
     const HeadOrder order(a.orders, h);
-    const T* base = a.in[2].row(b, h, 0);
+    const T* const base = a.in[2].row(b, h, 0);
     const int stride = a.in[2].token;
     LaneRow<T, D, false> next[IT];
     const auto read = [&](int blk) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
-            const int n_new = blk * BLK + it * ROWS + row;
-            int c0, c1, c2, n = order.source(min(n_new, t.n_img - 1), c0, c1, c2);
-            if (n_new >= t.n_img) n = min(n_new, a.n_tokens - 1);
-            next[it].load(base + (int64_t)n * stride, L);
-            if (n_new >= a.n_tokens) next[it].zero();
+            next[it].load(base + (int64_t)s.places.row[(blk - blk0) * BLK + it * ROWS + row].x * stride, L);
+            if (blk * BLK + it * ROWS + row >= a.n_tokens) next[it].zero();
         }
     };
+    s.places.fill(a, t, order, blk0, blk1 - blk0);
+    __syncthreads();
     read(blk0);
     for (int blk = blk0; blk < blk1; ++blk) {
-        const size_t group = (size_t)bh * a.kblocks + blk;
-        float y[IT][8], amax = 0.0f;
+        float y[IT][8], amax = 0.0f, scale = 1.0f;
 #pragma unroll
         for (int it = 0; it < IT; ++it)
 #pragma unroll
             for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e] = next[it][e]));
         if (blk + 1 < blk1) read(blk + 1);
-        float scale = 1.0f;
-        if constexpr (BITS != 16) {
-            amax = wave_max(amax);
-            if ((tid & 63) == 0) wave_amax[tid >> 6] = amax;
-            __syncthreads();
-#pragma unroll
-            for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, wave_amax[wave]);
-            if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
-        } else {
-            __syncthreads();
+        if (BITS != 16) {
+            amax = wavefront_max(amax);
+            if ((tid & 63) == 0) s.amax[tid >> 6] = amax;
         }
+        __syncthreads();  // also: the block before has left the staged tile
+        if constexpr (BITS != 16) {
+#pragma unroll
+            for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, s.amax[wave]);
+            amax = uniform(amax);
+            if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
+        }
+        const size_t group = (size_t)bh * a.kblocks + blk;
         if (tid == 0) a.scales[2][group] = scale;
         const GroupDivider quotient(scale);
 #pragma unroll
-        for (int it = 0; it < IT; ++it) stage_codes<BITS, BLK, D, false>(stage, it * ROWS + row, L, y[it], quotient);
+        for (int it = 0; it < IT; ++it) stage_codes<BITS, BLK, D, false>(s.stage, it * ROWS + row, L, y[it], quotient);
         __syncthreads();
-        store_staged<BITS, BLK, D>(a.codes[2] + group * OUT_BYTES, stage, tid);
+        store_staged<BITS, BLK, D>(a.codes[2] + group * OUT_BYTES, s.stage, tid);
     }
 }
 
+// grid: spans of blocks; batches x heads; Q, K, V
 template <typename T, int BLK, int D, int QKBITS, int PVBITS, bool HALVES, bool FOURS>
 __global__ __launch_bounds__(kThreads) void norm_rope_quantize_kernel(QuantArgs<T> a, Turning t, Norms norm) {
-    if (blockIdx.z < 2) quantize_rows<T, BLK, D, QKBITS, HALVES, FOURS>(a, t, norm, blockIdx.z);
-    else quantize_transposed<T, BLK, D, PVBITS>(a, t);
+    constexpr size_t rows = sizeof(RowsLds<BLK, D, HALVES>), transposed = sizeof(TransposedLds<BLK, D, PVBITS>);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[rows > transposed ? rows : transposed];
+    if (blockIdx.z < 2) quantize_rows<T, BLK, D, QKBITS, HALVES, FOURS>(a, t, norm, blockIdx.z, lds);
+    else quantize_transposed<T, BLK, D, PVBITS>(a, t, lds);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -968,8 +1039,11 @@ static int quantize_entry(const paro_shape* s, int64_t n, int64_t kb, int kind, 
     a.kblocks = (int)kb;
     a.nh = s->nh;
     a.kind = kind;
+    // As many blocks per workgroup as leave 2048 workgroups, eight for each compute unit: what a workgroup sets up is shared and all but its first
+    // block is read ahead (48 heads of 275 blocks, 8 bit: one block 182 us, two 160, eight 145 with an earlier form; 24 heads of 72, d = 128: with 4096
+    // workgroups 37.3, 2048 36.0, 1024 36.7).
     a.span = 1;
-    while (a.span < 8 && 3 * (int64_t)s->B * s->nh * ((kb + a.span) / (a.span + 1)) >= 4096) ++a.span;
+    while (a.span < kSpan && 3 * (int64_t)s->B * s->nh * ((kb + a.span) / (a.span + 1)) >= 2048) ++a.span;
     const auto run = pairs == PARO_PAIRS_HALVES ? (t.fours ? launch_quant<T, true, true> : launch_quant<T, true, false>)
                                                 : (t.fours ? launch_quant<T, false, true> : launch_quant<T, false, false>);
     if (!run(s, bits_qk, bits_pv, dim3((unsigned)((kb + a.span - 1) / a.span), (unsigned)(s->B * s->nh), 3), st, a, t, norm))
