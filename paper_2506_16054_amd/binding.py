@@ -142,7 +142,8 @@ def lib() -> ctypes.CDLL:
 # tokens is two calls and host work only, 9.3 us with it and 17.3 us through the checks below and ctypes.  It declines by
 # returning None whatever it does not take as it stands, and the function here goes on with its own checks.
 FASTCALL = ("paro_permute_quantize_qkv", "paro_permute_quantize_qkv_keep", "paro_sparse_attn", "paro_sparse_attn_unpermuted", "paro_unpermute",
-            "paro_mask_to_blocklist_device", "paro_permute_quantize_kv", "paro_permute_quantize_qkv_smoothed", "paro_sparse_attn_unpermuted_rawq")
+            "paro_mask_to_blocklist_device", "paro_permute_quantize_kv", "paro_permute_quantize_qkv_smoothed", "paro_sparse_attn_unpermuted_rawq",
+            "paro_rope", "paro_qk_norm_rope", "paro_qk_norm_rope_backward", "paro_qk_norm_rope_quantize_qkv")
 _fast = None
 
 
@@ -164,7 +165,8 @@ def _native():
         loader.exec_module(module)
         if module.built_for != torch.__version__:
             raise ParoError(PARO_EHIP, "%s is built for torch %s, not %s" % (path, module.built_for, torch.__version__))
-        module.bind(paro_shape, *(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in FASTCALL))
+        module.bind(paro_shape, paro_rope_axes, *(ctypes.cast(getattr(L, name), ctypes.c_void_p).value
+                                                  for name in (*FASTCALL, "paro_qk_norm_rope_backward_bytes")))
         _fast = module
     return _fast
 
@@ -654,7 +656,11 @@ class _Vectors:
         unknown = set(vectors) - set(self.NAMES)
         if unknown:
             raise ParoError(PARO_EINVAL, "unknown vector %s" % sorted(unknown)[0])
-        self.vectors = tuple(vectors.get(name) for name in self.NAMES)
+        self._vectors = tuple(vectors.get(name) for name in self.NAMES)
+
+    @property
+    def vectors(self):
+        return self._vectors
 
     def _fill(self, struct, d: int, dev: int) -> None:
         import torch
@@ -672,7 +678,15 @@ class QkNorm(_Vectors):
 
     def __init__(self, kind: int, eps: float = 1e-6, **vectors):
         super().__init__(**vectors)
-        self.kind, self.eps = int(kind), float(eps)
+        self._native = (int(kind), float(eps), *self._vectors)  # what the native module takes
+
+    @property
+    def kind(self) -> int:
+        return self._native[0]
+
+    @property
+    def eps(self) -> float:
+        return self._native[1]
 
     def struct(self, d: int, dev: int) -> paro_qk_norm:
         c = paro_qk_norm(kind=self.kind, eps=self.eps)
@@ -730,6 +744,8 @@ def _current_device(t) -> int:
 
 def paro_rope(s: paro_shape, axes: paro_rope_axes, table, x, y, inverse: bool = False) -> None:
     """x, y: [B, nh, N, d] float32 or bfloat16, any strides of whole 16-byte rows; y may be x.  inverse turns back (the gradient)."""
+    if _made((_fast or _layer_calls()).paro_rope(s, axes, table, x, y, inverse)):
+        return
     m, dev = _dims(s), _current_device(x)
     r = [_strided(t, name, m.x, x.dtype, dev) for name, t in (("x", x), ("y", y))]
     _check(lib().paro_rope(ctypes.byref(s), _dtype_code(x), ctypes.byref(axes), _rotation(s, axes, table, dev), int(bool(inverse)), *map(ctypes.byref, r),
@@ -737,6 +753,9 @@ def paro_rope(s: paro_shape, axes: paro_rope_axes, table, x, y, inverse: bool = 
 
 
 def paro_qk_norm_rope(s: paro_shape, axes: paro_rope_axes, table, norm: QkNorm, q, k, q_out, k_out) -> None:
+    """q, k, q_out, k_out: [B, nh, N, d], any strides of whole 16-byte rows; an output may be its input."""
+    if _made((_fast or _layer_calls()).paro_qk_norm_rope(s, axes, table, norm._native, q, k, q_out, k_out)):
+        return
     m, dev = _dims(s), _current_device(q)
     r = [_strided(t, name, m.x, q.dtype, dev) for name, t in (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out))]
     _check(lib().paro_qk_norm_rope(ctypes.byref(s), _dtype_code(q), ctypes.byref(axes), _rotation(s, axes, table, dev),
@@ -754,6 +773,9 @@ def paro_qk_norm_rope_backward(s: paro_shape, axes: paro_rope_axes, table, norm:
                                grad: Optional[QkNormGrad] = None, scratch=None) -> None:
     """dq_out, dk_out: gradients of the outputs; dq, dk receive those of q and k, `grad` those of the norms.  scratch: uint8
     [paro_qk_norm_rope_backward_bytes(s)], needed where grad holds a vector."""
+    if _made((_fast or _layer_calls()).paro_qk_norm_rope_backward(s, axes, table, norm._native, q, k, dq_out, dk_out, dq, dk,
+                                                              None if grad is None else grad._vectors, scratch)):
+        return
     import torch
 
     m, dev = _dims(s), _current_device(q)
@@ -771,6 +793,9 @@ def paro_qk_norm_rope_backward(s: paro_shape, axes: paro_rope_axes, table, norm:
 def paro_qk_norm_rope_quantize_qkv(s: paro_shape, bits_qk: int, bits_pv: int, perm_ids, axes: paro_rope_axes, table, norm: QkNorm, q, k, v,
                                    q_codes, sq, k_codes, sk, v_codes, sv) -> None:
     """paro_qk_norm_rope and paro_permute_quantize_qkv in one launch; q, k, v: [B, nh, N, d], any strides of whole 16-byte rows."""
+    if _made((_fast or _layer_calls()).paro_qk_norm_rope_quantize_qkv(s, bits_qk, bits_pv, perm_ids, axes, table, norm._native, q, k, v, q_codes, sq,
+                                                                  k_codes, sk, v_codes, sv)):
+        return
     import torch
 
     m, dev = _dims(s), _current_device(q)

@@ -25,6 +25,7 @@ namespace {
 
 // the library's entry points and the binding's shape type, handed over by the binding that has loaded the library
 PyTypeObject* g_shape;
+PyTypeObject* g_axes;
 decltype(&paro_permute_quantize_qkv) g_qkv;
 decltype(&paro_permute_quantize_qkv_keep) g_qkv_keep;
 decltype(&paro_sparse_attn) g_attn;
@@ -34,6 +35,11 @@ decltype(&paro_mask_to_blocklist_device) g_expand;
 decltype(&paro_permute_quantize_kv) g_kv;
 decltype(&paro_permute_quantize_qkv_smoothed) g_qkv_smoothed;
 decltype(&paro_sparse_attn_unpermuted_rawq) g_rawq;
+decltype(&paro_rope) g_rope;
+decltype(&paro_qk_norm_rope) g_norm_rope;
+decltype(&paro_qk_norm_rope_backward) g_norm_rope_backward;
+decltype(&paro_qk_norm_rope_quantize_qkv) g_norm_rope_quantize;
+decltype(&paro_qk_norm_rope_backward_bytes) g_backward_bytes;
 
 // What follows from a shape: as the binding's _Dims.
 struct Dims {
@@ -57,8 +63,8 @@ struct Dims {
     }
 };
 
-// A plain, contiguous tensor on the GPU.
-const at::Tensor* plain(PyObject* o) {
+// A plain tensor on the GPU, contiguous unless told otherwise.
+const at::Tensor* plain(PyObject* o, bool contiguous = true) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
     constexpr c10::DispatchKeySet wrapped({c10::DispatchKey::Python, c10::DispatchKey::PythonTLSSnapshot, c10::DispatchKey::Functionalize,
@@ -66,7 +72,7 @@ const at::Tensor* plain(PyObject* o) {
                                            c10::DispatchKey::FuncTorchBatchedDecomposition, c10::DispatchKey::FuncTorchDynamicLayerFrontMode,
                                            c10::DispatchKey::FuncTorchDynamicLayerBackMode, c10::DispatchKey::Batched, c10::DispatchKey::Conjugate,
                                            c10::DispatchKey::Negative, c10::DispatchKey::ZeroTensor});
-    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || t.key_set().has_any(wrapped) || !t.has_storage() || !t.is_contiguous())
+    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || t.key_set().has_any(wrapped) || !t.has_storage() || (contiguous && !t.is_contiguous()))
         return nullptr;
     return &t;
 }
@@ -122,6 +128,64 @@ bool number(PyObject* o, long* v) {
 }
 void* stream() { return (void*)c10::hip::getCurrentHIPStream().stream(); }
 void* ptr(const at::Tensor* t) { return t->data_ptr(); }
+
+// What the calls of norms and rotations share: shape, axes, table, the current device and its stream.
+struct Turn {
+    Dims m;
+    paro_rope_axes axes;
+    const at::Tensor* table = nullptr;
+    c10::hip::HIPStream current = c10::hip::getCurrentHIPStream();
+    bool here(const at::Tensor* t) const { return t && t->get_device() == current.device_index(); }
+    bool read(PyObject* s, PyObject* a, PyObject* t) {
+        if (!m.read(s) || Py_TYPE(a) != g_axes) return false;
+        Py_buffer b;
+        if (PyObject_GetBuffer(a, &b, PyBUF_SIMPLE) != 0) {
+            PyErr_Clear();
+            return false;
+        }
+        const bool ok = b.len == (Py_ssize_t)sizeof(axes);
+        if (ok) memcpy(&axes, b.buf, sizeof(axes));
+        PyBuffer_Release(&b);
+        if (!ok) return false;
+        const int64_t extent[3] = {m.s.F, m.s.Hg, m.s.Wg};
+        int64_t floats = 0;
+        for (int i = 0; i < 3; ++i) {
+            if (axes.dims[i] < 0 || axes.dims[i] % 2) return false;
+            floats += axes.dims[i] * extent[i];
+        }
+        return floats == 0 || here(table = typed(t, {floats / 2, 2}, at::kFloat));
+    }
+    // [B, nh, N, d] in any strides but the last
+    bool rows(PyObject* o, at::ScalarType type, paro_strided* r) const {
+        const at::Tensor* t = plain(o, false);
+        const int64_t shape[4] = {m.s.B, m.s.nh, m.n, m.s.d};
+        if (!here(t) || t->scalar_type() != type || !t->sizes().equals(c10::IntArrayRef(shape, 4)) || t->stride(3) != 1) return false;
+        *r = {t->data_ptr(), t->stride(0), t->stride(1), t->stride(2)};
+        return true;
+    }
+    // eight vectors [d] or None, in the order of paro_qk_norm; false unless every one is
+    bool vectors(PyObject* const* v, const float* (&to)[8]) const {
+        for (int i = 0; i < 8; ++i) {
+            const at::Tensor* t = v[i] == Py_None ? nullptr : typed(v[i], {m.s.d}, at::kFloat);
+            if (v[i] != Py_None && !here(t)) return false;
+            to[i] = t ? (const float*)t->data_ptr() : nullptr;
+        }
+        return true;
+    }
+    // (kind, eps, eight vectors)
+    bool norm(PyObject* o, paro_qk_norm* n) const {
+        const float* v[8];
+        long kind;
+        if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 10 || !number(PyTuple_GET_ITEM(o, 0), &kind) || !PyFloat_CheckExact(PyTuple_GET_ITEM(o, 1)) ||
+            !vectors(((PyTupleObject*)o)->ob_item + 2, v))
+            return false;
+        n->kind = (int)kind;
+        n->eps = PyFloat_AS_DOUBLE(PyTuple_GET_ITEM(o, 1));
+        for (int i = 0; i < 2; ++i) n->weight[i] = v[i], n->bias[i] = v[2 + i], n->text_weight[i] = v[4 + i], n->text_bias[i] = v[6 + i];
+        return true;
+    }
+    const float* angles() const { return table ? (const float*)table->data_ptr() : nullptr; }
+};
 
 // C++ exceptions (a tensor whose storage refuses, a device that is gone) must not cross into the interpreter.
 template <typename F>
@@ -335,6 +399,109 @@ PyObject* expand(PyObject* const* a, Py_ssize_t count) {  // nh, k, bitmask, row
     return PyLong_FromLong(status);
 }
 
+bool type_of(PyObject* o, at::ScalarType* type, paro_dtype* dtype) {
+    const at::Tensor* t = plain(o, false);
+    if (!t || !dtype_of(*t, dtype)) return false;
+    *type = t->scalar_type();
+    return true;
+}
+
+PyObject* rope(PyObject* const* a, Py_ssize_t count) {  // s, axes, table, x, y, inverse
+    if (count != 6 || !g_shape || !PyBool_Check(a[5])) PARO_DECLINE;
+    at::ScalarType type;
+    paro_dtype dtype;
+    if (!type_of(a[3], &type, &dtype)) PARO_DECLINE;
+    Turn t;
+    paro_strided x, y;
+    if (!t.read(a[0], a[1], a[2]) || !t.rows(a[3], type, &x) || !t.rows(a[4], type, &y)) PARO_DECLINE;
+    void* st = (void*)t.current.stream();
+    const int inverse = a[5] == Py_True;
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = g_rope(&t.m.s, dtype, &t.axes, t.angles(), inverse, &x, &y, st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
+PyObject* norm_rope(PyObject* const* a, Py_ssize_t count) {  // s, axes, table, (kind, eps, vectors), q, k, q_out, k_out
+    if (count != 8 || !g_shape) PARO_DECLINE;
+    at::ScalarType type;
+    paro_dtype dtype;
+    if (!type_of(a[4], &type, &dtype)) PARO_DECLINE;
+    Turn t;
+    paro_qk_norm norm;
+    paro_strided r[4];
+    if (!t.read(a[0], a[1], a[2]) || !t.norm(a[3], &norm)) PARO_DECLINE;
+    for (int i = 0; i < 4; ++i)
+        if (!t.rows(a[4 + i], type, &r[i])) PARO_DECLINE;
+    void* st = (void*)t.current.stream();
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = g_norm_rope(&t.m.s, dtype, &t.axes, t.angles(), &norm, r, r + 1, r + 2, r + 3, st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
+PyObject* norm_rope_backward(PyObject* const* a, Py_ssize_t count) {  // s, axes, table, norm, q, k, dq_out, dk_out, dq, dk, vectors or None, scratch or None
+    if (count != 12 || !g_shape) PARO_DECLINE;
+    at::ScalarType type;
+    paro_dtype dtype;
+    if (!type_of(a[4], &type, &dtype)) PARO_DECLINE;
+    Turn t;
+    paro_qk_norm norm;
+    paro_qk_norm_grad grad;
+    paro_strided r[6];
+    if (!t.read(a[0], a[1], a[2]) || !t.norm(a[3], &norm)) PARO_DECLINE;
+    for (int i = 0; i < 6; ++i)
+        if (!t.rows(a[4 + i], type, &r[i])) PARO_DECLINE;
+    if (a[10] != Py_None) {
+        const float* v[8];
+        if (!PyTuple_CheckExact(a[10]) || PyTuple_GET_SIZE(a[10]) != 8 || !t.vectors(((PyTupleObject*)a[10])->ob_item, v)) PARO_DECLINE;
+        for (int i = 0; i < 2; ++i)
+            grad.weight[i] = (float*)v[i], grad.bias[i] = (float*)v[2 + i], grad.text_weight[i] = (float*)v[4 + i], grad.text_bias[i] = (float*)v[6 + i];
+    }
+    const at::Tensor* scratch = nullptr;
+    if (a[11] != Py_None) {
+        const int64_t bytes = g_backward_bytes(&t.m.s);
+        if (bytes < 0 || !t.here(scratch = typed(a[11], {bytes}, at::kByte))) PARO_DECLINE;
+    }
+    void *st = (void*)t.current.stream(), *sp = scratch ? ptr(scratch) : nullptr;
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = g_norm_rope_backward(&t.m.s, dtype, &t.axes, t.angles(), &norm, r, r + 1, r + 2, r + 3, r + 4, r + 5, a[10] == Py_None ? nullptr : &grad, sp, st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
+PyObject* norm_rope_quantize(PyObject* const* a, Py_ssize_t count) {
+    // s, bits_qk, bits_pv, perm_ids, axes, table, norm, q, k, v, q_codes, sq, k_codes, sk, v_codes, sv
+    if (count != 16 || !g_shape) PARO_DECLINE;
+    at::ScalarType type;
+    paro_dtype dtype;
+    long qk, pv;
+    if (!number(a[1], &qk) || !number(a[2], &pv) || !type_of(a[7], &type, &dtype)) PARO_DECLINE;
+    Turn t;
+    PermIds ids;
+    paro_qk_norm norm;
+    paro_strided r[3];
+    if (!t.read(a[0], a[4], a[5]) || !ids.read(a[3], t.m.s.nh) || !t.norm(a[6], &norm)) PARO_DECLINE;
+    void* c[3];
+    float* f[3];
+    for (int i = 0; i < 3; ++i) {
+        const long bits = i == 2 ? pv : qk;
+        const at::Tensor *codes = i == 2 ? vt_of(a[14], t.m, bits) : rows_of(a[10 + 2 * i], t.m, bits), *scales = scales_of(a[11 + 2 * i], t.m);
+        if (!t.rows(a[7 + i], type, &r[i]) || !code_type(codes, bits) || !t.here(codes) || !t.here(scales)) PARO_DECLINE;
+        c[i] = ptr(codes);
+        f[i] = (float*)ptr(scales);
+    }
+    void* st = (void*)t.current.stream();
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = g_norm_rope_quantize(&t.m.s, dtype, (int)qk, (int)pv, ids.data(), &t.axes, t.angles(), &norm, r, r + 1, r + 2, c[0], f[0], c[1], f[1], c[2], f[2], st);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+
 PyObject* f_qkv(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return quantize_qkv(a, n, false); }); }
 PyObject* f_qkv_keep(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return quantize_qkv(a, n, true); }); }
 PyObject* f_attn(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return attention(a, n, false); }); }
@@ -345,12 +512,26 @@ PyObject* f_qkv_smoothed(PyObject*, PyObject* const* a, Py_ssize_t n) { return g
 PyObject* f_rawq(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return attention_rawq(a, n); }); }
 PyObject* f_expand(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return expand(a, n); }); }
 
-PyObject* f_bind(PyObject*, PyObject* args) {  // the shape type, then the addresses in the order of the declarations above
-    PyObject* shape;
-    unsigned long long p[9];
-    if (!PyArg_ParseTuple(args, "O!KKKKKKKKK", &PyType_Type, &shape, p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8)) return nullptr;
+PyObject* f_rope(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return rope(a, n); }); }
+PyObject* f_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return norm_rope(a, n); }); }
+PyObject* f_norm_rope_backward(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return norm_rope_backward(a, n); }); }
+PyObject* f_norm_rope_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) { return guarded([&] { return norm_rope_quantize(a, n); }); }
+
+PyObject* f_bind(PyObject*, PyObject* args) {  // the types of shapes and axes, then the addresses in the order of the declarations above
+    PyObject *shape, *axes;
+    unsigned long long p[14];
+    if (!PyArg_ParseTuple(args, "O!O!KKKKKKKKKKKKKK", &PyType_Type, &shape, &PyType_Type, &axes, p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8,
+                          p + 9, p + 10, p + 11, p + 12, p + 13))
+        return nullptr;
     Py_INCREF(shape);  // for the life of the process, like the library
+    Py_INCREF(axes);
     g_shape = (PyTypeObject*)shape;
+    g_axes = (PyTypeObject*)axes;
+    g_rope = (decltype(g_rope))(uintptr_t)p[9];
+    g_norm_rope = (decltype(g_norm_rope))(uintptr_t)p[10];
+    g_norm_rope_backward = (decltype(g_norm_rope_backward))(uintptr_t)p[11];
+    g_norm_rope_quantize = (decltype(g_norm_rope_quantize))(uintptr_t)p[12];
+    g_backward_bytes = (decltype(g_backward_bytes))(uintptr_t)p[13];
     g_qkv = (decltype(g_qkv))(uintptr_t)p[0];
     g_qkv_keep = (decltype(g_qkv_keep))(uintptr_t)p[1];
     g_attn = (decltype(g_attn))(uintptr_t)p[2];
@@ -374,6 +555,10 @@ PyMethodDef methods[] = {
     {"paro_permute_quantize_kv", (PyCFunction)(void (*)(void))f_kv, METH_FASTCALL, nullptr},
     {"paro_permute_quantize_qkv_smoothed", (PyCFunction)(void (*)(void))f_qkv_smoothed, METH_FASTCALL, nullptr},
     {"paro_sparse_attn_unpermuted_rawq", (PyCFunction)(void (*)(void))f_rawq, METH_FASTCALL, nullptr},
+    {"paro_rope", (PyCFunction)(void (*)(void))f_rope, METH_FASTCALL, nullptr},
+    {"paro_qk_norm_rope", (PyCFunction)(void (*)(void))f_norm_rope, METH_FASTCALL, nullptr},
+    {"paro_qk_norm_rope_backward", (PyCFunction)(void (*)(void))f_norm_rope_backward, METH_FASTCALL, nullptr},
+    {"paro_qk_norm_rope_quantize_qkv", (PyCFunction)(void (*)(void))f_norm_rope_quantize, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "paro_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

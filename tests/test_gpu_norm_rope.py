@@ -21,6 +21,14 @@ def _pb():
     return pb
 
 
+@pytest.fixture(params=["native", "ctypes"], autouse=True)
+def route(request, monkeypatch):
+    """Every call through the native module, which must take it, and through the binding's own checks and ctypes."""
+    pb = _pb()
+    monkeypatch.setattr(pb, "_fast", pb._native() if request.param == "native" else pb._NoNative)
+    return request.param
+
+
 class Problem:
     """Inputs on the device in some memory layout, and the same values in float64 on the host."""
 
@@ -402,6 +410,34 @@ def test_streams_and_graphs(what):
         torch.cuda.synchronize()
         after = [*out] if what == "forward" else [*out, *grads.values()] if what == "backward" else [*codes, *scales]
         assert all(torch.equal(a, b) for a, b in zip(after, want)), seed
+
+
+def test_the_native_module_takes_the_calls():
+    """What it is made for it does not leave to the binding."""
+    import torch
+
+    pb = _pb()
+    f = pb._native()
+    for layout in ("heads", "fused"):
+        p = Problem(kind="layer", T=3, text_norm=True, layout=layout)
+        out, dy = p.empty(2), p.rows(2)
+        grads = pb.QkNormGrad(**{name: torch.empty((64,), device="cuda:0") for name in p.vectors})
+        scratch = torch.empty((pb.paro_qk_norm_rope_backward_bytes(p.s),), dtype=torch.uint8, device="cuda:0")
+        codes, scales = _buffers(pb, p.s, 8, 4, 0)
+        ids = np.array([0, 1, 2], np.uint8)
+        assert f.paro_rope(p.s, p.axes, p.table, p.x[0], out[0], True) == pb.PARO_OK
+        assert f.paro_qk_norm_rope(p.s, p.axes, p.table, p.norm._native, *p.x[:2], *out) == pb.PARO_OK
+        assert f.paro_qk_norm_rope_backward(p.s, p.axes, p.table, p.norm._native, *p.x[:2], *dy, *out, grads._vectors, scratch) == pb.PARO_OK
+        assert f.paro_qk_norm_rope_backward(p.s, p.axes, p.table, p.norm._native, *p.x[:2], *dy, *out, None, None) == pb.PARO_OK
+        assert f.paro_qk_norm_rope_quantize_qkv(p.s, 8, 4, ids, p.axes, p.table, p.norm._native, *p.x, codes[0], scales[0], codes[1], scales[1], codes[2],
+                                                scales[2]) == pb.PARO_OK
+        # and declines what the binding refuses
+        for bad in (p.x[0].cpu(), p.x[0].half(), p.x[0][..., ::2], p.x[0][:, :, 1:], None):
+            assert f.paro_rope(p.s, p.axes, p.table, bad, out[0], False) is None
+            assert f.paro_qk_norm_rope(p.s, p.axes, p.table, p.norm._native, p.x[0], bad, *out) is None
+        assert f.paro_rope(p.s, p.axes, p.table[1:], p.x[0], out[0], False) is None and f.paro_rope(p.s, p.s, p.table, p.x[0], out[0], False) is None
+        assert f.paro_qk_norm_rope(p.s, p.axes, p.table, p.norm._native[:-1], *p.x[:2], *out) is None
+        assert f.paro_qk_norm_rope_backward(p.s, p.axes, p.table, p.norm._native, *p.x[:2], *dy, *out, grads._vectors, scratch[:-4]) is None
 
 
 def test_refusals_of_the_binding():
