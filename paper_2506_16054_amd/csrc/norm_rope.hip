@@ -3,13 +3,19 @@
 //
 // A row is the d channels of one token of one head.  d / 8 lanes share it, eight channels each: for adjacent pairs the eight
 // from 8 L on, for pairs across the halves four from 4 L on and the four that lie d / 2 behind them, so that a lane holds both
-// channels of its pairs 4 L .. 4 L + 3.  Row sums meet across neighbouring lanes (DPP); nothing goes through LDS.
+// channels of its pairs 4 L .. 4 L + 3.  Row sums meet across neighbouring lanes (DPP).  (16 channels a lane: 183 vector registers, two wavefronts
+// per SIMD, 126 us where eight take 91.)
 //
 // The angles' table separates by axis: some KB instead of some MB per layer, so it comes from the caches nearest to the compute
 // unit.
 //
 // Sums and values are binary64 and rounded to binary32 once: the codes of the quantizing form then do not depend on the order of
-// a sum (up to values within 2^-50 of a rounding border).
+// a sum (up to values within 2^-45 of a rounding border), and the instructions cost what binary32 ones do.
+//
+// Everything but the 8- and 4-bit quantizing form is bound by HBM.  48 heads of 17550 bf16 tokens, d = 64, where a copy takes 5.2 TB/s: rotation 45
+// us (216 MB, 4.8 TB/s) out of one projection's output and 39 from contiguous heads, norms and rotation of Q and K 91 (431 MB, 4.7) and 82,
+// gradients 143 (647 MB, 4.5) and 131.  Stores past the caches take 5 to 15 % off these kernels by themselves, and add more than that to the next one, which
+// reads what they wrote (copy, norms and rotation, quantizer: 323 -> 329 us; 24 heads of 4608 tokens, d = 128: 46.0 -> 47.8): not used.
 #include <math.h>
 #include <string.h>
 
@@ -28,7 +34,7 @@ struct Turning {
     int pairs[3];  // pairs per axis
     int base[3];   // first entry of an axis in the table
     int total;     // pairs that turn; pair p turns with the axis whose run of pairs holds it
-    bool fours;    // every axis has a multiple of four pairs: four consecutive entries from a multiple of four on are one axis' and 32 aligned bytes
+    bool fours;    // there are pairs, a multiple of four per axis: four entries from a multiple of four on are one axis' and 32 aligned bytes
     int n_img, Hg, Wg;
     double inv_hg, inv_wg;
     float sign;  // -1: turned back
@@ -52,6 +58,10 @@ struct Rows {
 // floor(n / divisor) for 0 <= n < 2^24 and a divisor of at most that, inv = fl64(1 / divisor): (n + 1/2) inv lies 1 / (2 divisor)
 // or more from the next integers, and is off by less than 2^-51 n / divisor.
 __device__ inline int quotient_of(int n, double inv) { return (int)(((double)n + 0.5) * inv); }
+
+// By value: a conditional between members would choose between their addresses, and every lane would load from there.
+__device__ __forceinline__ int pick(int c0, int c1, int c2, int place) { return place == 0 ? c0 : place == 1 ? c1 : c2; }
+__device__ __forceinline__ const float* pick(const float* image, const float* text, bool is_text) { return is_text ? text : image; }
 
 // ---- the 8 channels of a lane --------------------------------------------------------------------------------------
 typedef unsigned uint4v __attribute__((ext_vector_type(4)));
@@ -291,8 +301,9 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(RowsArgs<T> a, Tu
     LaneTurn angles;
     turn_of_token(t, L, n, angles);
     float w[8], bias[8];
-    if constexpr (KIND != PARO_NORM_NONE) load_vector<D, HALVES>(norm.w[z][n >= t.n_img], L, 1.0f, w);
-    if constexpr (KIND == PARO_NORM_LAYER) load_vector<D, HALVES>(norm.b[z][n >= t.n_img], L, 0.0f, bias);
+    const bool text = n >= t.n_img;
+    if constexpr (KIND != PARO_NORM_NONE) load_vector<D, HALVES>(pick(norm.w[z][0], norm.w[z][1], text), L, 1.0f, w);
+    if constexpr (KIND == PARO_NORM_LAYER) load_vector<D, HALVES>(pick(norm.b[z][0], norm.b[z][1], text), L, 0.0f, bias);
     for (int h = h0; h < h1; ++h) {
         const LaneRow<T, D, HALVES> x = next;
         if (h + 1 < h1) next.load(a.in[z].row(b, h + 1, n), L);
@@ -332,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_grad_kernel(GradArgs<T> a,
         next_dy.load(a.dy[z].row(b, h0, n), L);
         LaneTurn angles;
         turn_of_token(t, L, n, angles);
-            float w[8];
+        float w[8];
         load_vector<D, HALVES>(norm.w[z][text], L, 1.0f, w);
         for (int h = h0; h < h1; ++h) {
             const Lane x = next_x, dy = next_dy;
@@ -591,9 +602,6 @@ struct HeadOrder {
     }
 };
 
-// by value: a conditional between members would choose between their addresses, and load from there
-__device__ __forceinline__ int pick(int c0, int c1, int c2, int place) { return place == 0 ? c0 : place == 1 ? c1 : c2; }
-
 // Where a lane's angles lie in the table when its four pairs belong to one axis (Turning::fours).
 struct LaneAxis {
     int place, pairs, base;  // base < 0: the lane's pairs do not turn
@@ -844,7 +852,7 @@ static int make_turning(const paro_shape* s, const paro_rope_axes* axes, const f
     if (t->total && !table) return fail(PARO_EINVAL, "table is NULL");
     if (misaligned(table)) return fail(PARO_EINVAL, "table must be 16-byte aligned");
     t->table = table;
-    t->fours = true;
+    t->fours = t->total > 0;  // kernels may read four entries for a lane that does not turn
     const int extent[3] = {s->F, s->Hg, s->Wg};
     int64_t at = 0;
     for (int a = 0; a < 3; ++a) {

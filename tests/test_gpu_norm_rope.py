@@ -263,7 +263,8 @@ def test_rows_of_zeros_and_what_is_not_finite():
 QUANT = [
     dict(), dict(block=32), dict(d=128, kind="layer", T=64, text_norm=True, grid=(1, 8, 8)), dict(d=128, block=32, kind="rms", halves=1, dims=(44, 42, 42)),
     dict(kind="layer", layout="fused", grid=(3, 7, 11), nh=6), dict(kind="none", layout="tokens", halves=1, T=5, grid=(1, 5, 7)),
-    dict(B=1, nh=1, grid=(1, 1, 1)), dict(B=1, nh=2, grid=(1, 1, 65), block=64, dims=(8, 10, 4)), dict(B=1, nh=12, grid=(5, 9, 10), dims=(20, 22, 22), kind="layer"),
+    dict(B=1, nh=1, grid=(1, 1, 1)), dict(B=1, nh=2, grid=(1, 1, 65), block=64, dims=(8, 10, 4)), dict(kind="layer", dims=(0, 0, 0), T=3),
+    dict(kind="none", dims=(0, 0, 0)), dict(dims=(8, 8, 8), T=70, text_norm=True), dict(d=128, dims=(0, 0, 64), halves=1), dict(B=1, nh=12, grid=(5, 9, 10), dims=(20, 22, 22), kind="layer"),
 ]
 
 
