@@ -195,6 +195,8 @@ def test_backward(case):
     grads = {name: torch.full((p.d,), 5.0, device="cuda:0") for name in (p.vectors if p.vectors or p.kind == "none" else ("q_weight", "k_weight"))}
     scratch = torch.full((pb.paro_qk_norm_rope_backward_bytes(p.s),), 255, dtype=torch.uint8, device="cuda:0")  # NaN wherever it is read unwritten
     pb.paro_qk_norm_rope_backward(p.s, p.axes, p.table, p.norm, p.x[0], p.x[1], *dy, *dx, pb.QkNormGrad(**grads), scratch)
+    if p.layout == "fused":  # the slice that is not an output is left as it was
+        assert bool((p.whole[:, :, 2] == 7).all())
     spans = {"": slice(0, p.n_img), "text_": slice(p.n_img, None)}
     for i, which in enumerate("qk"):
         x, g = host(p.x[i]), host(dy[i])
@@ -474,6 +476,106 @@ def test_refusals_of_the_binding():
         pb.paro_qk_norm_rope_quantize_qkv(p.s, 8, 4, [0, 1, 2], p.axes, p.table, p.norm, *p.x, codes[0], scales[0], codes[1], scales[1], codes[2], scales[2])
     with pytest.raises(pb.ParoError):
         pb.paro_qk_norm_rope_quantize_qkv(p.s, 8, 8, [0, 1, 9], p.axes, p.table, p.norm, *p.x, codes[0], scales[0], codes[1], scales[1], codes[2], scales[2])
+
+
+def _between(shape, dtype, mark):
+    """A tensor with 64 marked elements in front of it and behind it, and a check that they are still there."""
+    import torch
+
+    n = int(np.prod(shape))
+    whole = torch.full((n + 128,), mark, dtype=dtype, device="cuda:0")
+    return whole[64: 64 + n].view(shape), lambda: bool((whole[:64] == mark).all()) and bool((whole[64 + n:] == mark).all())
+
+
+@pytest.mark.parametrize("case", [dict(d=64, kind="layer", grid=(1, 5, 13), T=3), dict(d=128, kind="rms", grid=(1, 1, 1)), dict(d=64, kind="rms", block=32, grid=(3, 7, 5))],
+                         ids=_id)
+def test_nothing_beside_the_outputs_is_written(case):
+    import torch
+
+    pb = _pb()
+    p = Problem(B=1, nh=3, dtype="float32", **case)
+    intact, make = [], lambda shape, dtype, mark: (lambda t, ok: (intact.append(ok), t)[1])(*_between(shape, dtype, mark))
+    shape = (1, 3, p.n, p.d)
+    out = [make(shape, torch.float32, 7.0) for _ in range(2)]
+    pb.paro_rope(p.s, p.axes, p.table, p.x[0], out[0])
+    pb.paro_qk_norm_rope(p.s, p.axes, p.table, p.norm, *p.x[:2], *out)
+    grads = {name: make((p.d,), torch.float32, 7.0) for name in p.vectors}
+    scratch = make((pb.paro_qk_norm_rope_backward_bytes(p.s),), torch.uint8, 7)
+    pb.paro_qk_norm_rope_backward(p.s, p.axes, p.table, p.norm, *p.x[:2], *p.rows(2), *out, pb.QkNormGrad(**grads), scratch)
+    for bits in ((8, 8), (4, 4), (16, 16)):
+        ct = torch.bfloat16 if bits[0] == 16 else torch.int8
+        codes = [make(pb.codes_shape(p.s, bits[0], lay), ct, 7) for lay in (pb.PARO_ROWS, pb.PARO_ROWS, pb.PARO_VT)]
+        scales = [make((1, 3, pb.paro_nblocks(p.s)), torch.float32, 7.0) for _ in range(3)]
+        pb.paro_qk_norm_rope_quantize_qkv(p.s, *bits, [0, 3, 5], p.axes, p.table, p.norm, *p.x, codes[0], scales[0], codes[1], scales[1], codes[2], scales[2])
+    assert all(ok() for ok in intact)
+
+
+def test_two_streams_at_once():
+    """Two gradients at the same time, each with a scratch of its own, give what each gives alone."""
+    import torch
+
+    pb = _pb()
+    problems = [Problem(B=1, nh=8, grid=(4, 16, 17), kind="layer", dtype="float32", seed=s) for s in (1, 2)]
+    work = []
+    for p in problems:
+        grads = {name: torch.empty((p.d,), device="cuda:0") for name in p.vectors}
+        scratch = torch.empty((pb.paro_qk_norm_rope_backward_bytes(p.s),), dtype=torch.uint8, device="cuda:0")
+        work.append((p, p.rows(2), p.empty(2), grads, scratch))
+
+    def call(p, dy, dx, grads, scratch):
+        pb.paro_qk_norm_rope_backward(p.s, p.axes, p.table, p.norm, *p.x[:2], *dy, *dx, pb.QkNormGrad(**grads), scratch)
+
+    want = []
+    for w in work:
+        call(*w)
+        want.append([t.clone() for t in (*w[2], *w[3].values())])
+    streams = [torch.cuda.Stream() for _ in work]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, w in zip(streams, work):
+            with torch.cuda.stream(stream):
+                call(*w)
+    torch.cuda.synchronize()
+    for w, ref in zip(work, want):
+        assert all(torch.equal(a, b) for a, b in zip((*w[2], *w[3].values()), ref))
+
+
+@pytest.mark.parametrize("grid,T", [((1, 1, 1 << 20), 13), ((1 << 20, 1, 1), 0), ((3, 1021, 349), 70)])
+def test_long_sequences(grid, T):
+    """A million tokens: sampled rows against the oracle, the codes of one head against the two calls."""
+    import torch
+
+    pb = _pb()
+    d, dims, n = 64, (16, 24, 24), int(np.prod(grid)) + T
+    s, axes = pb.make_shape(1, 1, d, *grid, T, 64), pb.make_rope_axes((16, 24, 24))
+    pos = [np.arange(x, dtype=np.float64) for x in grid]
+    freq = [10000.0 ** (-np.arange(0, x, 2, dtype=np.float64) / x) for x in dims]
+    h_table = pb.paro_rope_table(s, axes, pos, freq)
+    table, norm = torch.from_numpy(h_table).to("cuda:0"), pb.QkNorm(pb.PARO_NORM_RMS, 1e-6)
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    q, k, v = (torch.randn((1, 1, n, d), generator=gen, device="cuda:0") for _ in range(3))
+    out = [torch.empty_like(q) for _ in range(2)]
+    pb.paro_qk_norm_rope(s, axes, table, norm, q, k, *out)
+    rng = np.random.default_rng(5)
+    rows = np.unique(np.concatenate([[0, 1, n // 2, n - T - 1, n - 1], rng.integers(0, n, 200)]))
+    cos, sin = np.ones((len(rows), d // 2)), np.zeros((len(rows), d // 2))
+    for i, row in enumerate(rows):
+        if row < n - T:
+            coords, p, base = (row // (grid[1] * grid[2]), row // grid[2] % grid[1], row % grid[2]), 0, 0
+            for c, extent, dim in zip(coords, grid, dims):
+                part = h_table[base + c * (dim // 2): base + (c + 1) * (dim // 2)]
+                cos[i, p: p + dim // 2], sin[i, p: p + dim // 2] = part[:, 0], part[:, 1]
+                p, base = p + dim // 2, base + extent * (dim // 2)
+    at = torch.from_numpy(rows).to("cuda:0")
+    for x, y in zip((q, k), out):
+        check_values(y[0, 0, at], on.norm_rope(host(x[0, 0, at]), "rms", 1e-6, 1.0, 0.0, cos, sin, 0), torch.float32, "rows")
+    for order in (1, 5):
+        got, gs = _buffers(pb, s, 8, 8, 2)
+        want, ws = _buffers(pb, s, 8, 8, 1)
+        pb.paro_qk_norm_rope_quantize_qkv(s, 8, 8, [order], axes, table, norm, q, k, v, got[0], gs[0], got[1], gs[1], got[2], gs[2])
+        pb.paro_permute_quantize_qkv(s, 8, 8, [order], *out, v, want[0], ws[0], want[1], ws[1], want[2], ws[2])
+        for i in range(3):
+            assert torch.equal(got[i], want[i]) and torch.equal(gs[i], ws[i]), (order, i)
 
 
 def test_offsets_beyond_32_bits():
