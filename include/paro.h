@@ -315,7 +315,8 @@ int paro_rope_table(const paro_shape* s, const paro_rope_axes* axes, const doubl
 /* Rows of d consecutive channels on the device, the row of batch b, head h, token n at element
  * b * batch + h * head + n * token of `data`: [B,nh,N,d], [B,N,nh,d] or a slice of a fused projection [B,N,3,nh,d].
  * Every row starts at a multiple of 16 bytes.  Strides are not negative, the token's is below 2^31; rows that are written
- * do not overlap (batch, head and token strides, sorted, each span what the smaller ones cover). */
+ * do not overlap (batch, head and token strides, sorted, each span what the smaller ones cover).  What a call writes
+ * overlaps nothing else that it is given, but for the exact coincidences that it allows. */
 typedef struct paro_strided {
     void* data;
     int64_t batch, head, token;

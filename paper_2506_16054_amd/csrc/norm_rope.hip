@@ -4,7 +4,7 @@
 // A row is the d channels of one token of one head.  d / 8 lanes share it, eight channels each: for adjacent pairs the eight
 // from 8 L on, for pairs across the halves four from 4 L on and the four that lie d / 2 behind them, so that a lane holds both
 // channels of its pairs 4 L .. 4 L + 3.  Row sums meet across neighbouring lanes (DPP).  (16 channels a lane: 183 vector registers, two wavefronts
-// per SIMD, 126 us where eight take 91.)
+// per SIMD, 126 us where eight take 89.)
 //
 // The angles' table separates by axis: some KB instead of some MB per layer, so it comes from the caches nearest to the compute
 // unit.
@@ -12,9 +12,9 @@
 // Sums and values are binary64 and rounded to binary32 once: the codes of the quantizing form then do not depend on the order of
 // a sum (up to values within 2^-45 of a rounding border), and the instructions cost what binary32 ones do.
 //
-// Everything but the 8- and 4-bit quantizing form is bound by HBM.  48 heads of 17550 bf16 tokens, d = 64, where a copy takes 5.2 TB/s: rotation 45
-// us (216 MB, 4.8 TB/s) out of one projection's output and 39 from contiguous heads, norms and rotation of Q and K 91 (431 MB, 4.7) and 82,
-// gradients 143 (647 MB, 4.5) and 131.  Stores past the caches take 5 to 15 % off these kernels by themselves, and add more than that to the next one, which
+// Everything but the 8- and 4-bit quantizing form is bound by HBM.  48 heads of 17550 bf16 tokens, d = 64, where a copy takes 5.2 TB/s: rotation 44
+// us (216 MB, 4.9 TB/s) out of one projection's output and 39 from contiguous heads, norms and rotation of Q and K 89 (431 MB, 4.8) and 81,
+// gradients 142 (647 MB, 4.6) and 130.  Stores past the caches take 5 to 15 % off these kernels by themselves, and add more than that to the next one, which
 // reads what they wrote (copy, norms and rotation, quantizer: 323 -> 329 us; 24 heads of 4608 tokens, d = 128: 46.0 -> 47.8): not used.
 #include <math.h>
 #include <string.h>
@@ -674,9 +674,9 @@ struct TransposedLds {
 // registers between the pass for the largest value and the codes.
 //
 // Bound by vector instructions with 8-bit codes (some 200 for the eight channels of a lane, a third of them binary64), by HBM with bf16.
-// 48 heads of 17550 bf16 tokens, d = 64, layer norms, out of one projection's output: 123 us with 8-bit codes (485 MB), 135 with bf16 (647 MB, 4.8 TB/s); one
+// 48 heads of 17550 bf16 tokens, d = 64, layer norms, out of one projection's output: 122 us with 8-bit codes (485 MB), 133 with bf16 (647 MB, 4.9 TB/s); one
 // block per workgroup, no reading ahead, each row's place found by all of its lanes, weights in registers: 192 and 190.  Q and K in one
-// workgroup, for their common places and angles: 6 % more registers, slower by 3 %.
+// workgroup, for their common places and angles: 116 registers in place of 90, 3 % slower.
 template <typename T, int BLK, int D, int BITS, bool HALVES, bool FOURS>
 __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turning& t, const Norms& norm, int z, uint8_t* lds) {
     constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
@@ -905,7 +905,7 @@ static int heads_per_group(const paro_shape* s, int64_t tiles, int tensors, int 
 // Forward: four workgroups for each compute unit before anything else.  With fewer heads a workgroup's angles and weights cost more than
 // its rows (24 heads of 4608 tokens, d = 128, rotation: one head 15.1 us, three 11.9, six 11.5), with more a launch ends unevenly (48
 // heads of 17550 tokens, d = 64, rotation: three 44.8, six 46.2, twelve 49.8; Q and K with root-mean-square norms six 86.8, twelve 88.0, 24
-// 90.6; with layer norms, which hold more per lane, six 93.8, twelve 91.5, 24 94.6).
+// 90.6; with layer norms, which hold more per lane, in the form of the day six 93.8, twelve 91.5, 24 94.6).
 static int forward_heads(const paro_shape* s, int64_t tiles, int tensors, int kind) {
     return heads_per_group(s, tiles, tensors, 1024, kind == PARO_NORM_LAYER ? 4096 : 8192);
 }
