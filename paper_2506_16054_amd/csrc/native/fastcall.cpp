@@ -415,10 +415,11 @@ PyObject* rope(PyObject* const* a, Py_ssize_t count) {  // s, axes, table, x, y,
     paro_strided x, y;
     if (!t.read(a[0], a[1], a[2]) || !t.rows(a[3], type, &x) || !t.rows(a[4], type, &y)) PARO_DECLINE;
     void* st = (void*)t.current.stream();
+    const float* angles = t.angles();
     const int inverse = a[5] == Py_True;
     int status;
     Py_BEGIN_ALLOW_THREADS;
-    status = g_rope(&t.m.s, dtype, &t.axes, t.angles(), inverse, &x, &y, st);
+    status = g_rope(&t.m.s, dtype, &t.axes, angles, inverse, &x, &y, st);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(status);
 }
@@ -435,9 +436,10 @@ PyObject* norm_rope(PyObject* const* a, Py_ssize_t count) {  // s, axes, table, 
     for (int i = 0; i < 4; ++i)
         if (!t.rows(a[4 + i], type, &r[i])) PARO_DECLINE;
     void* st = (void*)t.current.stream();
+    const float* angles = t.angles();
     int status;
     Py_BEGIN_ALLOW_THREADS;
-    status = g_norm_rope(&t.m.s, dtype, &t.axes, t.angles(), &norm, r, r + 1, r + 2, r + 3, st);
+    status = g_norm_rope(&t.m.s, dtype, &t.axes, angles, &norm, r, r + 1, r + 2, r + 3, st);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(status);
 }
@@ -466,9 +468,10 @@ PyObject* norm_rope_backward(PyObject* const* a, Py_ssize_t count) {  // s, axes
         if (bytes < 0 || !t.here(scratch = typed(a[11], {bytes}, at::kByte))) PARO_DECLINE;
     }
     void *st = (void*)t.current.stream(), *sp = scratch ? ptr(scratch) : nullptr;
+    const float* angles = t.angles();
     int status;
     Py_BEGIN_ALLOW_THREADS;
-    status = g_norm_rope_backward(&t.m.s, dtype, &t.axes, t.angles(), &norm, r, r + 1, r + 2, r + 3, r + 4, r + 5, a[10] == Py_None ? nullptr : &grad, sp, st);
+    status = g_norm_rope_backward(&t.m.s, dtype, &t.axes, angles, &norm, r, r + 1, r + 2, r + 3, r + 4, r + 5, a[10] == Py_None ? nullptr : &grad, sp, st);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(status);
 }
@@ -495,9 +498,10 @@ PyObject* norm_rope_quantize(PyObject* const* a, Py_ssize_t count) {
         f[i] = (float*)ptr(scales);
     }
     void* st = (void*)t.current.stream();
+    const float* angles = t.angles();
     int status;
     Py_BEGIN_ALLOW_THREADS;
-    status = g_norm_rope_quantize(&t.m.s, dtype, (int)qk, (int)pv, ids.data(), &t.axes, t.angles(), &norm, r, r + 1, r + 2, c[0], f[0], c[1], f[1], c[2], f[2], st);
+    status = g_norm_rope_quantize(&t.m.s, dtype, (int)qk, (int)pv, ids.data(), &t.axes, angles, &norm, r, r + 1, r + 2, c[0], f[0], c[1], f[1], c[2], f[2], st);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(status);
 }

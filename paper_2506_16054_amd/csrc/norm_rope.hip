@@ -22,7 +22,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "quantize_tile.h"
+#include "common.h"
 
 namespace paro {
 
@@ -527,18 +527,19 @@ template <int BITS, int BLK, int D, bool HALVES>
 __device__ __forceinline__ void stage_codes(uint8_t* stage, int token, int L, const float (&x)[8], const GroupDivider& quotient) {
     typedef LaneRow<float, D, HALVES> Lane;
     const int slot = vt_slot(token);
-    int q[8];
+    const auto at = [&](int e) { return (Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)) * stage_row<BITS, BLK>() + slot; };
     if constexpr (BITS == 16) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q[e] = f32_to_bf16_bits(x[e]);
+        for (int e = 0; e < 8; e += 2) {
+            const unsigned two = pack_bf16(x[e], x[e + 1]);
+            ((uint16_t*)stage)[at(e)] = (uint16_t)two;
+            ((uint16_t*)stage)[at(e + 1)] = (uint16_t)(two >> 16);
+        }
     } else {
+        int q[8];
         codes_of<BITS>(x, quotient, q);
-    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int at = (Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)) * stage_row<BITS, BLK>() + slot;
-        if constexpr (BITS == 16) ((uint16_t*)stage)[at] = (uint16_t)q[e];
-        else stage[at] = (uint8_t)q[e];
+        for (int e = 0; e < 8; ++e) stage[at(e)] = (uint8_t)q[e];
     }
 }
 
