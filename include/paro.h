@@ -379,8 +379,8 @@ int paro_qk_norm_rope_backward(const paro_shape* s, paro_dtype dtype, const paro
                                const paro_strided* dk, const paro_qk_norm_grad* grad, void* scratch, void* stream);
 
 /* paro_qk_norm_rope to float32 followed by paro_permute_quantize_qkv of its outputs and v, in one launch and without
- * the intermediate tensors: codes and scales are those of the two calls bit for bit (with float32 v; bfloat16 v is
- * widened, which is exact).
+ * the intermediate tensors: codes and scales are those of the two calls bit for bit for finite values (with float32 v;
+ * bfloat16 v is widened, which is exact).
  *   q, k, v      rows of dtype, default token order
  *   (bits_qk, bits_pv), h_perm_ids, *_codes, s*: as paro_permute_quantize_qkv */
 int paro_qk_norm_rope_quantize_qkv(const paro_shape* s, paro_dtype dtype, int bits_qk, int bits_pv, const uint8_t* h_perm_ids,
