@@ -257,7 +257,8 @@ __device__ __forceinline__ void turn_lane(V (&u)[8], const LaneTurn& t) {
     }
 }
 
-// The row behind norm and rotation, rounded to binary32.  w and b: 1 and -0 where there is nothing (exact, signs of zeros included).
+// The row behind norm and rotation, rounded to binary32.  w and b: 1 and 0 where there is nothing, in every kernel: a row that is its mean then
+// leaves +0 under any weights.
 template <typename T, int D, bool HALVES, typename W>
 __device__ __forceinline__ void normed_and_turned(const LaneRow<T, D, HALVES>& x, int kind, double eps, const W& w, const W& b, const LaneTurn& t,
                                                   float (&y)[8]) {
@@ -646,7 +647,7 @@ struct Vectors {
             const int which = __builtin_amdgcn_readfirstlane((threadIdx.x + j * kThreads) / D), c = threadIdx.x % D, bias = which & 1, text = which >> 1;
             const float* p = bias ? norm.b[z][text] : norm.w[z][text];
             const int L = HALVES ? c % (D / 2) / 4 : c / 8, e = HALVES ? c % 4 + (c >= D / 2 ? 4 : 0) : c % 8;
-            v[text][bias][((e >> 1) * LANES + L) * 2 + (e & 1)] = p ? (double)p[c] : bias ? -0.0 : 1.0;
+            v[text][bias][((e >> 1) * LANES + L) * 2 + (e & 1)] = p ? (double)p[c] : bias ? 0.0 : 1.0;
         }
     }
 };

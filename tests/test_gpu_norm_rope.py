@@ -310,6 +310,38 @@ def test_quantize(case, dtype, bits):
         assert np.array_equal(gs[0][0, h].cpu().numpy(), scales) and np.array_equal(got[0][0, h].cpu().numpy(), codes), h
 
 
+@pytest.mark.parametrize("weight,bias", [(None, None), (-1.5, None), (-1.5, 0.0), (1.5, -0.0)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_signs_of_zeros(kind, weight, bias):
+    """Rows that are their mean, rows of zeros of either sign: bf16 codes are those of the two calls in every bit, and so are the forward
+    call's zeros: a bias that is not there is a zero, as one that is."""
+    import torch
+
+    pb = _pb()
+    p = Problem(kind=kind, ones=True, dtype="float32", T=5, dims=(8, 0, 16), grid=(2, 3, 11))
+    for i, x in enumerate(p.x[:2]):
+        x[..., 0::4, :], x[..., 1::4, :], x[..., 2::4, :] = 0.0, -0.0, 0.5 - i
+    vectors = {}
+    for name, value in (("weight", weight), ("bias", bias)):
+        if value is not None and (name == "weight" or kind == "layer"):
+            vectors.update({x + "_" + name: torch.full((p.d,), value, device="cuda:0") for x in "qk"})
+    norm = pb.QkNorm(pb.PARO_NORM_RMS if kind == "rms" else pb.PARO_NORM_LAYER, 1e-6, **vectors)
+    ids = np.array([0, 3, 5], np.uint8)
+    got, gs = _buffers(pb, p.s, 16, 16, 2)
+    pb.paro_qk_norm_rope_quantize_qkv(p.s, 16, 16, ids, p.axes, p.table, norm, *p.x, got[0], gs[0], got[1], gs[1], got[2], gs[2])
+    out = p.empty(2)
+    pb.paro_qk_norm_rope(p.s, p.axes, p.table, norm, p.x[0], p.x[1], *out)
+    want, ws = _buffers(pb, p.s, 16, 16, 1)
+    pb.paro_permute_quantize_qkv(p.s, 16, 16, ids, *out, p.x[2], want[0], ws[0], want[1], ws[1], want[2], ws[2])
+    for i in range(3):
+        off = int((got[i].view(torch.int16) != want[i].view(torch.int16)).sum())
+        assert off == 0, (i, off)
+    if kind == "layer" and bias is None:
+        for y in out:
+            still = y[..., p.n_img:, :]  # text does not turn: (x - m) r w + 0, never -0
+            assert not torch.any((still == 0) & torch.signbit(still))
+
+
 @pytest.mark.parametrize("case", [dict(d=64, kind="layer", layout="fused"), dict(d=128, kind="rms", halves=1, dims=(44, 42, 42)), dict(d=64, kind="none", block=32)], ids=_id)
 def test_quantize_many_blocks(case):
     """Workgroups that go through several blocks, from image tokens into text: the codes and scales of the two calls."""
