@@ -462,15 +462,55 @@ __device__ __forceinline__ float wavefront_max(float v) {
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// The largest magnitude of a lane's values: past every NaN, or NaN where there is one (v_maximum3_f32, which needs its operands in no
+// canonical form first).
+template <bool NANS, int N>
+__device__ __forceinline__ float lane_max(const float (&y)[N][8]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int it = 0; it < N; ++it)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = NANS ? __builtin_elementwise_maximum(m, fabsf(y[it][e])) : fmaxf(m, fabsf(y[it][e]));
+    return m;
+}
+
 __device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
 
+// x / scale for a group as GroupDivider has it, correctly rounded, with short ways to the scale amax / QMAX (the same theorem, with the constant's
+// reciprocal) and to 1 / scale: from the instruction's estimate y, within a unit in the last place, 1 - scale y is exact, and y + y (1 - scale y)
+// rounds correctly for every significand but all ones.  Both equal the divide for each amax of the range (all 10^9 compared).
+// nans: there are some among the wavefront's values; its quotients then take the divide and its clamps.
 template <int BITS>
-__device__ __forceinline__ void codes_of(const float (&x)[8], const GroupDivider& quotient, int (&q)[8]) {
-    constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
+struct GroupQuotient {
+    static constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
+    float scale, inv;
+    bool generic;
+    __device__ __forceinline__ GroupQuotient(float amax, bool nans) {
+        constexpr float INV = 1.0f / QMAX;
+        if (amax > 1e-18f && amax < 1e20f) {
+            const float q0 = amax * INV;
+            scale = fmaf(fmaf(-q0, QMAX, amax), INV, q0);
+            const float y = __builtin_amdgcn_rcpf(scale);
+            inv = fmaf(fmaf(-scale, y, 1.0f), y, y);
+            generic = nans || (__float_as_uint(scale) & 0x7fffffu) == 0x7fffffu;
+        } else {
+            scale = amax > 0.0f ? amax / QMAX : 1.0f;
+            inv = 0.0f;
+            generic = true;
+        }
+    }
+};
+
+// Codes of a lane's values, each in the low byte (4-bit codes: the low four bits) of its word.  A quotient of numbers is at most QMAX (1 + 2^-22) in
+// magnitude where the scale is a normal number, which rounds to QMAX: only the generic divide clamps, in groups whose scale lost bits or is
+// infinite, and NaN.  Adding 1.5 2^23 rounds to an integer, halves to even, and leaves it as two's complement in the low bits.
+template <int BITS>
+__device__ __forceinline__ void codes_of(const float (&x)[8], const GroupQuotient<BITS>& quotient, unsigned (&q)[8]) {
+    constexpr float QMAX = GroupQuotient<BITS>::QMAX;
     float r[8];
     if (quotient.generic) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = x[e] / quotient.scale;
+        for (int e = 0; e < 8; ++e) r[e] = fminf(fmaxf(x[e] / quotient.scale, -QMAX), QMAX);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -479,12 +519,17 @@ __device__ __forceinline__ void codes_of(const float (&x)[8], const GroupDivider
         }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = (int)fminf(fmaxf(rintf(r[e]), -QMAX), QMAX);  // v_rndne_f32: round half to even
+    for (int e = 0; e < 8; ++e) q[e] = __float_as_uint(r[e] + 12582912.0f);
+}
+
+// The low bytes of four words.
+__device__ __forceinline__ unsigned low_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
 }
 
 // PARO_ROWS: a lane's codes into its row of the group.
 template <int BITS, int D, bool HALVES>
-__device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x)[8], const GroupDivider& quotient) {
+__device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x)[8], const GroupQuotient<BITS>& quotient) {
     typedef LaneRow<float, D, HALVES> Lane;
     const int first = Lane::first(L), second = first + Lane::SECOND;
     if constexpr (BITS == 16) {
@@ -496,13 +541,10 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x
             *(uint4v*)(row + 2 * first) = (uint4v){v[0], v[1], v[2], v[3]};
         }
     } else {
-        int q[8];
+        unsigned q[8];
         codes_of<BITS>(x, quotient, q);
+        unsigned v[2] = {low_bytes(q[0], q[1], q[2], q[3]), low_bytes(q[4], q[5], q[6], q[7])};
         if constexpr (BITS == 8) {
-            unsigned v[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                v[i] = (q[4 * i] & 0xff) | ((q[4 * i + 1] & 0xff) << 8) | ((q[4 * i + 2] & 0xff) << 16) | ((unsigned)q[4 * i + 3] << 24);
             if constexpr (HALVES) {
                 *(unsigned*)(row + first) = v[0];
                 *(unsigned*)(row + second) = v[1];
@@ -510,14 +552,15 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x
                 *(uint2v*)(row + first) = (uint2v){v[0], v[1]};
             }
         } else {
-            unsigned v = 0;
+            // bytes 0 and 2 of each word take their upper neighbour's code as upper half
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v |= (unsigned)(q[e] & 0xf) << (4 * e);
+            for (int i = 0; i < 2; ++i) v[i] = (v[i] & 0x000f000f) | (v[i] >> 4 & 0x00f000f0);
+            const unsigned all = __builtin_amdgcn_perm(v[1], v[0], 0x06040200);
             if constexpr (HALVES) {
-                *(uint16_t*)(row + first / 2) = (uint16_t)v;
-                *(uint16_t*)(row + second / 2) = (uint16_t)(v >> 16);
+                *(uint16_t*)(row + first / 2) = (uint16_t)all;
+                *(uint16_t*)(row + second / 2) = (uint16_t)(all >> 16);
             } else {
-                *(unsigned*)(row + first / 2) = v;
+                *(unsigned*)(row + first / 2) = all;
             }
         }
     }
@@ -525,7 +568,7 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int L, const float (&x
 
 // PARO_VT: a lane's channels of token `token` of the block, into the staged tile.
 template <int BITS, int BLK, int D, bool HALVES>
-__device__ __forceinline__ void stage_codes(uint8_t* stage, int token, int L, const float (&x)[8], const GroupDivider& quotient) {
+__device__ __forceinline__ void stage_codes(uint8_t* stage, int token, int L, const float (&x)[8], const GroupQuotient<BITS>& quotient) {
     typedef LaneRow<float, D, HALVES> Lane;
     const int slot = vt_slot(token);
     const auto at = [&](int e) { return (Lane::first(L) + (e >> 2) * Lane::SECOND + (e & 3)) * stage_row<BITS, BLK>() + slot; };
@@ -537,7 +580,7 @@ __device__ __forceinline__ void stage_codes(uint8_t* stage, int token, int L, co
             ((uint16_t*)stage)[at(e + 1)] = (uint16_t)(two >> 16);
         }
     } else {
-        int q[8];
+        unsigned q[8];
         codes_of<BITS>(x, quotient, q);
 #pragma unroll
         for (int e = 0; e < 8; ++e) stage[at(e)] = (uint8_t)q[e];
@@ -682,7 +725,6 @@ struct TransposedLds {
 template <typename T, int BLK, int D, int BITS, bool HALVES, bool FOURS>
 __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turning& t, const Norms& norm, int z, uint8_t* lds) {
     constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
-    constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
     RowsLds<BLK, D, HALVES>& s = *(RowsLds<BLK, D, HALVES>*)lds;
     const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
     const int blk0 = blockIdx.x * a.span, blk1 = min(blk0 + a.span, a.kblocks);
@@ -734,11 +776,12 @@ __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turni
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[it][e] = 0.0f;
             }
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) amax = fmaxf(fmaxf(amax, fabsf(y[it][e])), fabsf(y[it][e + 1]));
         }
-        float scale = 1.0f;
+        bool nans = false;
         if constexpr (BITS != 16) {
+            amax = lane_max<true>(y);
+            nans = __any(amax != amax);
+            if (nans) amax = lane_max<false>(y);
             amax = wavefront_max(amax);
             float* meet = s.amax[blk & 1];  // of two in turn: this one was read before the last block's barrier
             if ((tid & 63) == 0) meet[tid >> 6] = amax;
@@ -746,11 +789,10 @@ __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turni
 #pragma unroll
             for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, meet[wave]);
             amax = uniform(amax);
-            if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
         }
         const size_t group = (size_t)bh * a.kblocks + blk;
-        if (tid == 0) a.scales[z][group] = scale;
-        const GroupDivider quotient(scale);
+        const GroupQuotient<BITS> quotient(amax, nans);
+        if (tid == 0) a.scales[z][group] = quotient.scale;
         uint8_t* out = a.codes[z] + group * OUT_BYTES;
 #pragma unroll
         for (int it = 0; it < IT; ++it) store_codes<BITS, D, HALVES>(out + (it * ROWS + row) * (D * BITS / 8), L, y[it], quotient);
@@ -761,7 +803,6 @@ __device__ __forceinline__ void quantize_rows(const QuantArgs<T>& a, const Turni
 template <typename T, int BLK, int D, int BITS>
 __device__ __forceinline__ void quantize_transposed(const QuantArgs<T>& a, const Turning& t, uint8_t* lds) {
     constexpr int LANES = D / 8, ROWS = kThreads / LANES, IT = BLK / ROWS, OUT_BYTES = BLK * D * BITS / 8, WAVES = kThreads / 64;
-    constexpr float QMAX = BITS == 4 ? 7.0f : 127.0f;
     TransposedLds<BLK, D, BITS>& s = *(TransposedLds<BLK, D, BITS>*)lds;
     const int tid = threadIdx.x, L = tid % LANES, row = tid / LANES, bh = blockIdx.y, b = bh / a.nh, h = bh - b * a.nh;
     const int blk0 = blockIdx.x * a.span, blk1 = min(blk0 + a.span, a.kblocks);
@@ -780,13 +821,17 @@ __device__ __forceinline__ void quantize_transposed(const QuantArgs<T>& a, const
     __syncthreads();
     read(blk0);
     for (int blk = blk0; blk < blk1; ++blk) {
-        float y[IT][8], amax = 0.0f, scale = 1.0f;
+        float y[IT][8], amax = 0.0f;
+        bool nans = false;
 #pragma unroll
         for (int it = 0; it < IT; ++it)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[it][e] = next[it][e]));
+            for (int e = 0; e < 8; ++e) y[it][e] = next[it][e];
         if (blk + 1 < blk1) read(blk + 1);
-        if (BITS != 16) {
+        if constexpr (BITS != 16) {
+            amax = lane_max<true>(y);
+            nans = __any(amax != amax);
+            if (nans) amax = lane_max<false>(y);
             amax = wavefront_max(amax);
             if ((tid & 63) == 0) s.amax[tid >> 6] = amax;
         }
@@ -795,11 +840,10 @@ __device__ __forceinline__ void quantize_transposed(const QuantArgs<T>& a, const
 #pragma unroll
             for (int wave = 0; wave < WAVES; ++wave) amax = fmaxf(amax, s.amax[wave]);
             amax = uniform(amax);
-            if (amax > 0.0f) scale = amax / QMAX;  // correctly rounded binary32 divide
         }
         const size_t group = (size_t)bh * a.kblocks + blk;
-        if (tid == 0) a.scales[2][group] = scale;
-        const GroupDivider quotient(scale);
+        const GroupQuotient<BITS> quotient(amax, nans);
+        if (tid == 0) a.scales[2][group] = quotient.scale;
 #pragma unroll
         for (int it = 0; it < IT; ++it) stage_codes<BITS, BLK, D, false>(s.stage, it * ROWS + row, L, y[it], quotient);
         __syncthreads();

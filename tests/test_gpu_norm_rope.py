@@ -342,6 +342,61 @@ def test_signs_of_zeros(kind, weight, bias):
             assert not torch.any((still == 0) & torch.signbit(still))
 
 
+def _same_as_two_calls(p, ids, bits, x):
+    """Codes and scales of x, which neither norm nor rotation changes, against those of paro_permute_quantize_qkv, in every bit."""
+    import torch
+
+    pb = _pb()
+    got, gs = _buffers(pb, p.s, *bits, 2)
+    pb.paro_qk_norm_rope_quantize_qkv(p.s, *bits, ids, p.axes, p.table, p.norm, *x, got[0], gs[0], got[1], gs[1], got[2], gs[2])
+    want, ws = _buffers(pb, p.s, *bits, 1)
+    pb.paro_permute_quantize_qkv(p.s, *bits, ids, *x, want[0], ws[0], want[1], ws[1], want[2], ws[2])
+    for i in range(3):
+        off = (got[i] != want[i]).flatten(3).any(-1), gs[i].view(torch.int32) != ws[i].view(torch.int32)
+        assert not any(bool(o.any()) for o in off), (i, [o.nonzero()[:4].tolist() for o in off])
+
+
+@pytest.mark.parametrize("bits", [(8, 8), (8, 4), (4, 4), (4, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_of_any_size(d, bits):
+    """Blocks of every binary exponent: the smallest subnormals, scales whose significand is all ones, the largest numbers; values half a
+    step from a code among the others."""
+    import torch
+
+    p = Problem(B=1, nh=6, d=d, kind="none", grid=(1, 1, 32 * 277), dims=(0, 0, 0), dtype="float32", block=32)
+    r = p.rng
+    for x in p.x:
+        exponent = np.arange(277) - 149  # 2^-149 .. 2^127
+        top = np.ldexp(1 + r.random((6, 277)), exponent).astype(np.float32)
+        qmax = 7.0 if bits[0] == 4 else 127.0
+        top[5] = (np.ldexp(2 - 2.0**-23, exponent - 8) * qmax).astype(np.float32)  # amax / qmax is all ones, or next to it
+        v = (r.random((6, 277, 32, d)) * 2 - 1) * top[..., None, None]
+        halves = np.rint(r.random((6, 277, 32, d)) * 2 * qmax - qmax - 0.5) + 0.5
+        v = np.where(r.random(v.shape) < 0.3, halves * (top / np.float32(qmax)).astype(np.float64)[..., None, None], v)
+        v = np.clip(v, -top[..., None, None].astype(np.float64), top[..., None, None].astype(np.float64)).astype(np.float32)
+        v[:, :, 7, 3] = -top
+        x.copy_(torch.from_numpy(v.reshape(1, 6, 277 * 32, d)))
+        assert bool(torch.isfinite(x).all())
+    _same_as_two_calls(p, np.zeros(6, np.uint8), bits, p.x)
+
+
+@pytest.mark.parametrize("bits", [(8, 8), (4, 4)])
+@pytest.mark.parametrize("block", [32, 64])
+def test_codes_of_what_is_not_finite(block, bits):
+    """NaN and infinities in a block, one or a whole wavefront of them, without a norm: the scale and codes of paro_permute_quantize_qkv."""
+    p = Problem(B=1, nh=3, kind="none", grid=(3, 8, 16), T=5, dims=(0, 0, 0), dtype="float32", block=block)
+    nan, inf = float("nan"), float("inf")
+    for i, x in enumerate(p.x):
+        x[0, 0, 17 + i, 5] = nan
+        x[0, 0, 70:78] = nan
+        x[0, 1, 3] = -nan
+        x[0, 1, 100, 63], x[0, 1, 101, 0] = inf, nan
+        x[0, 2, 130:200] = nan
+        x[0, 2, 300, 1] = -inf
+        x[0, 2, -1] = nan
+    _same_as_two_calls(p, np.array([0, 2, 5], np.uint8), bits, p.x)
+
+
 @pytest.mark.parametrize("case", [dict(d=64, kind="layer", layout="fused"), dict(d=128, kind="rms", halves=1, dims=(44, 42, 42)), dict(d=64, kind="none", block=32)], ids=_id)
 def test_quantize_many_blocks(case):
     """Workgroups that go through several blocks, from image tokens into text: the codes and scales of the two calls."""
