@@ -718,8 +718,8 @@ struct TransposedLds {
 // Q (z = 0) or K: one workgroup goes through `span` blocks of a head and reads a block while it works on the one before; the block stays in
 // registers between the pass for the largest value and the codes.
 //
-// Bound by vector instructions with 8-bit codes (some 200 for the eight channels of a lane, a third of them binary64), by HBM with bf16.
-// 48 heads of 17550 bf16 tokens, d = 64, layer norms, out of one projection's output: 122 us with 8-bit codes (485 MB), 133 with bf16 (647 MB, 4.9 TB/s); one
+// Bound by vector instructions with 8-bit codes (some 180 for the eight channels of a lane, V's among them; a third binary64), by HBM with bf16.
+// 48 heads of 17550 bf16 tokens, d = 64, layer norms, out of one projection's output: 117 us with 8-bit codes (485 MB, 4.1 TB/s), 133 with bf16 (647 MB, 4.9 TB/s); one
 // block per workgroup, no reading ahead, each row's place found by all of its lanes, weights in registers: 192 and 190.  Q and K in one
 // workgroup, for their common places and angles: 116 registers in place of 90, 3 % slower.
 template <typename T, int BLK, int D, int BITS, bool HALVES, bool FOURS>
